@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int, c_size_t, c_uint64, c_void_p
+from ctypes import POINTER, c_char_p, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 import numpy as np
 
@@ -54,6 +54,10 @@ class vla_block_weights(ctypes.Structure):
 class vla_boundary(ctypes.Structure):
     _fields_ = [("hidden", c_void_p), ("hidden_bytes", c_size_t), ("kv", c_void_p), ("kv_bytes", c_size_t),
                 ("out_dtype", c_int), ("frame_id", c_uint64)]
+
+
+class vla_heads(ctypes.Structure):
+    _fields_ = [("p", c_void_p), ("seq", c_int64), ("token", c_int64), ("head", c_int64)]
 
 
 class vla_vision_cfg(ctypes.Structure):
@@ -113,6 +117,18 @@ def lib():
             "vla_op_gemm_route": [c_int, c_int, c_int, c_int, c_int, P(c_int), P(c_int), P(c_int)],
             "vla_op_gemm_tile_bf16": [c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int,
                                       c_int, c_void_p],
+            "vla_op_w4_pack": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
+            "vla_op_gemv_w4": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int, c_int,
+                               c_int, c_int, c_void_p],
+            "vla_op_qk_norm_rope": [P(vla_heads), P(vla_heads), c_int, c_void_p, c_void_p, c_float, c_void_p, c_void_p,
+                                    c_int, c_void_p, P(vla_heads), P(vla_heads), c_int, c_int, c_int, c_int, c_int,
+                                    c_void_p],
+            "vla_op_kv4_store": [P(vla_heads), P(vla_heads), c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int,
+                                 c_int, c_void_p],
+            "vla_op_kv4_load": [c_void_p, c_void_p, c_void_p, P(vla_heads), P(vla_heads), c_int, c_int, c_int, c_int,
+                                c_int, c_void_p],
+            "vla_op_attention_kv4": [P(vla_heads), c_void_p, c_void_p, P(vla_heads), c_int, c_int, c_int, c_int, c_int,
+                                     c_int, c_int, c_int, c_int, c_void_p, c_size_t, c_void_p],
             "vla_suffix_create": [P(vla_stack_cfg), c_int, c_int, c_int, P(c_void_p)],
             "vla_suffix_load_block_weights": [c_void_p, c_int, P(vla_block_weights)],
             "vla_suffix_run": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
@@ -136,6 +152,9 @@ def lib():
             fn.restype = c_int
         L.vla_op_packed_weight_elems.argtypes = [c_int, c_int]
         L.vla_op_packed_weight_elems.restype = c_size_t
+        for name, n in (("vla_op_w4_packed_bytes", 3), ("vla_op_kv4_bytes", 4), ("vla_op_attention_kv4_scratch", 8)):
+            getattr(L, name).argtypes = [c_int] * n
+            getattr(L, name).restype = c_size_t
         L.vla_status_string.argtypes = [c_int]
         L.vla_status_string.restype = c_char_p
         L.vla_last_error.argtypes = [c_void_p]
@@ -395,6 +414,158 @@ def vla_op_gemm_route(op, M, N, K, a_parts=1):
 
 def vla_op_gemm_tile_bf16(op, tile, A, Wp, out, bias, M, N, K, stream=None):
     _check(lib().vla_op_gemm_tile_bf16(op, *tile, _ptr(A), _ptr(Wp), _ptr(out), _ptr(bias), M, N, K, stream))
+
+
+# ----------------------------------------- 4-bit weights and KV cache (torch)
+# These calls take torch tensors on the GPU and read sizes and strides off
+# them; a tensor whose type, shape or size does not fit raises ValueError
+# before the library is called.  `stream`: a hipStream_t (torch's
+# `stream.cuda_stream`), None = the null stream.
+
+_DTYPES = {}
+
+
+def _dtype(t):
+    """VLA_BF16 or VLA_F32 of a tensor."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: VLA_BF16, torch.float32: VLA_F32})
+    return _DTYPES.get(t.dtype, -1)
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dev(t, like, what):
+    """Address of a dense tensor on `like`'s device (None: NULL)."""
+    if t is None:
+        return None
+    _need(t.is_contiguous() and t.device == like.device, "%s: a contiguous tensor on %s is needed" % (what, like.device))
+    return t.data_ptr()
+
+
+def _int32(t, like, shape, what):
+    """Address of a dense int32 device tensor of that shape (None: NULL)."""
+    if t is None:
+        return None
+    _need(t.element_size() == 4 and not t.is_floating_point() and tuple(t.shape) == shape, "%s: int32 %s is needed" % (what, shape))
+    return _dev(t, like, what)
+
+
+def _f32(t, like, shape, what):
+    """Address of a dense fp32 device tensor of that shape (None: NULL)."""
+    if t is None:
+        return None
+    _need(_dtype(t) == VLA_F32 and tuple(t.shape) == shape, "%s: float32 %s is needed" % (what, shape))
+    return _dev(t, like, what)
+
+
+def _heads(t, shape, like, what, dtype=VLA_BF16):
+    """vla_heads over a tensor [B, tokens, heads, dh] of any outer strides."""
+    _need(tuple(t.shape) == shape and _dtype(t) == dtype and t.device == like.device and t.is_cuda,
+          "%s: %s %s on the GPU is needed" % (what, "float32" if dtype == VLA_F32 else "bfloat16", shape))
+    s = t.stride()
+    _need(s[3] == 1, "%s: the last dimension has to be dense" % what)
+    # the stride of a dimension of one is never used
+    return vla_heads(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+
+
+def vla_op_w4_packed_bytes(N, K, group):
+    return lib().vla_op_w4_packed_bytes(N, K, group)
+
+
+def vla_op_w4_pack(codes, scales, zeros, Wp, group, stream=None):
+    """codes [N, K] uint8, scales and zeros (or None) [N, ceil(K / group)]
+    bfloat16 -> Wp, a uint8 tensor of vla_op_w4_packed_bytes(N, K, group)."""
+    _need(codes.dim() == 2 and codes.element_size() == 1 and codes.is_cuda, "codes: uint8 [N, K] on the GPU is needed")
+    N, K = codes.shape
+    need = vla_op_w4_packed_bytes(N, K, group)
+    for t, what in ((scales, "scales"), (zeros, "zeros")):
+        _need(t is None or (_dtype(t) == VLA_BF16 and tuple(t.shape) == (N, -(-K // max(group, 1)))),
+              "%s: bfloat16 [N, ceil(K / group)] is needed" % what)
+    _need(Wp.numel() * Wp.element_size() >= need, "Wp: %d bytes are needed" % need)
+    _check(lib().vla_op_w4_pack(_dev(codes, codes, "codes"), _dev(scales, codes, "scales"), _dev(zeros, codes, "zeros"),
+                                _dev(Wp, codes, "Wp"), N, K, group, stream))
+
+
+def vla_op_gemv_w4(x, Wp, residual, out, N, group, swiglu=False, stream=None):
+    """x [M, K] bfloat16 and residual (None or float32), out [M, N or N / 2]
+    (float32 or bfloat16), rows of any stride; residual's rows and out's are
+    equally far apart."""
+    _need(x.dim() == 2 and _dtype(x) == VLA_BF16 and x.stride(1) == 1 and x.is_cuda, "x: bfloat16 [M, K] on the GPU is needed")
+    M, K = x.shape
+    wide = (M, N // 2 if swiglu else N)
+    _need(tuple(out.shape) == wide and out.stride(1) == 1 and _dtype(out) >= 0 and out.device == x.device,
+          "out: float32 or bfloat16 %s is needed" % (wide,))
+    ldo = out.stride(0) if M > 1 else 0
+    res = None
+    if residual is not None:
+        _need(tuple(residual.shape) == wide and _dtype(residual) == VLA_F32 and residual.stride(1) == 1
+              and residual.device == x.device and (M == 1 or residual.stride(0) == ldo),
+              "residual: float32 %s with out's row stride is needed" % (wide,))
+        res = residual.data_ptr()
+    _need(Wp.numel() * Wp.element_size() >= vla_op_w4_packed_bytes(N, K, group), "Wp: not the packed weights of these sizes")
+    _check(lib().vla_op_gemv_w4(x.data_ptr(), x.stride(0) if M > 1 else 0, _dev(Wp, x, "Wp"), res, out.data_ptr(), ldo,
+                                _dtype(out), int(swiglu), M, N, K, group, stream))
+
+
+def vla_op_qk_norm_rope(q, k, gq, gk, eps, cos, sin, pos, q_out, k_out, stream=None):
+    """q, q_out [B, L, H, dh], k, k_out [B, L, Hkv, dh] (inputs bfloat16 or
+    float32, outputs bfloat16), gq, gk [dh] and cos, sin [n_pos, dh / 2]
+    float32 or None, pos [B, L] int32 or None."""
+    _need(q.dim() == 4 and k.dim() == 4 and q.is_cuda, "q, k: [B, L, heads, dh] on the GPU are needed")
+    B, L, H, dh = q.shape
+    kshape = (B, L, k.shape[2], dh)
+    n_pos = 0 if cos is None else cos.shape[0]
+    dt = _dtype(q)
+    _check(lib().vla_op_qk_norm_rope(_heads(q, (B, L, H, dh), q, "q", dt), _heads(k, kshape, q, "k", dt), dt,
+                                     _f32(gq, q, (dh,), "gq"), _f32(gk, q, (dh,), "gk"), eps,
+                                     _f32(cos, q, (n_pos, dh // 2), "cos"), _f32(sin, q, (n_pos, dh // 2), "sin"), n_pos,
+                                     _int32(pos, q, (B, L), "pos"), _heads(q_out, (B, L, H, dh), q, "q_out"),
+                                     _heads(k_out, kshape, q, "k_out"), B, L, H, k.shape[2], dh, stream))
+
+
+def vla_op_kv4_bytes(B, Hkv, L_cap, dh):
+    return lib().vla_op_kv4_bytes(B, Hkv, L_cap, dh)
+
+
+def _kv4_rows(k, v, start, count, cache, L_cap):
+    _need(k.dim() == 4 and k.is_cuda, "k: [B, L, Hkv, dh] on the GPU is needed")
+    B, L, Hkv, dh = shape = tuple(k.shape)
+    _need(cache.numel() * cache.element_size() >= vla_op_kv4_bytes(B, Hkv, L_cap, dh), "cache: not of these sizes")
+    return (_heads(k, shape, k, "k"), _heads(v, shape, k, "v"), _int32(start, k, (B,), "start"),
+            _int32(count, k, (B,), "count"), _dev(cache, k, "cache"), (B, L, Hkv, L_cap, dh))
+
+
+def vla_op_kv4_store(k, v, start, count, cache, L_cap, stream=None):
+    """k, v [B, L, Hkv, dh] bfloat16, start, count [B] int32 or None, cache a
+    uint8 tensor of vla_op_kv4_bytes(B, Hkv, L_cap, dh)."""
+    k, v, start, count, cache, sizes = _kv4_rows(k, v, start, count, cache, L_cap)
+    _check(lib().vla_op_kv4_store(k, v, start, count, cache, *sizes, stream))
+
+
+def vla_op_kv4_load(cache, L_cap, start, count, k, v, stream=None):
+    """The inverse of vla_op_kv4_store, into k and v."""
+    k, v, start, count, cache, sizes = _kv4_rows(k, v, start, count, cache, L_cap)
+    _check(lib().vla_op_kv4_load(cache, start, count, k, v, *sizes, stream))
+
+
+def vla_op_attention_kv4_scratch(B, Lq, H, Hkv, dh, max_len, window=0, sinks=0):
+    return lib().vla_op_attention_kv4_scratch(B, Lq, H, Hkv, dh, max_len, window, sinks)
+
+
+def vla_op_attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window=0, sinks=0, scratch=None, stream=None):
+    """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a uint8 tensor of
+    vla_op_attention_kv4_scratch(...) bytes (None where that is 0)."""
+    _need(q.dim() == 4 and q.is_cuda and lens is not None, "q [B, Lq, H, dh] and lens [B] on the GPU are needed")
+    B, Lq, H, dh = shape = tuple(q.shape)
+    _need(cache.numel() * cache.element_size() >= vla_op_kv4_bytes(B, Hkv, L_cap, dh), "cache: not of these sizes")
+    nbytes = 0 if scratch is None else scratch.numel() * scratch.element_size()
+    _check(lib().vla_op_attention_kv4(_heads(q, shape, q, "q"), _dev(cache, q, "cache"), _int32(lens, q, (B,), "lens"),
+                                      _heads(o, shape, q, "o"), B, Lq, H, Hkv, L_cap, dh, max_len, window, sinks,
+                                      _dev(scratch, q, "scratch") if nbytes else None, nbytes, stream))
 
 
 def vla_status_string(code: int) -> str:

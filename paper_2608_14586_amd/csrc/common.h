@@ -38,4 +38,4 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
-static inline int cdiv(int a, int b) { return (a + b - 1) / b; }
+static constexpr inline int cdiv(int a, int b) { return (a + b - 1) / b; }

@@ -148,6 +148,63 @@ hipError_t decode_up(const float* h, const float* g, float eps, const WOperand& 
 hipError_t decode_down(const bf16_t* a, int fpad, const WOperand& W, float* h, int B, int N, hipStream_t s,
                        int parts = 1);
 
+// ------------------------------------------------- 4-bit weights and KV cache
+// Head rows of a call: element (b, token, head, d) at p + b * seq + token *
+// this->token + head * this->head + d, strides in elements.
+struct Heads {
+  void* p;
+  int64_t seq, token, head;
+};
+
+// Packed 4-bit weights (w4.hip): codes [N][K] one a byte (low four bits),
+// scales and zeros [N][ceil(K / group)] bf16 (zeros NULL: 8), group in {32, 64, 128}.
+size_t w4_packed_bytes(int N, int K, int group);
+hipError_t w4_pack(const uint8_t* codes, const bf16_t* scales, const bf16_t* zeros, void* wp, int N, int K, int group,
+                   hipStream_t s);
+// out[M][N] (fp32 or bf16) = x W^T + res (fp32 [M][ldo], NULL: none);
+// swiglu: out[M][N / 2] = silu(x Wg^T) * (x Wu^T) + res, Wg the first N / 2
+// rows of W, N % 32 == 0.  K % 8 == 0, ldx % 8 == 0.
+hipError_t gemv_w4(const bf16_t* x, int64_t ldx, const void* wp, const float* res, void* out, int64_t ldo, bool f32,
+                   bool swiglu, int M, int N, int K, int group, hipStream_t s);
+
+// Per-head RMS norm and rotary embedding (qk_norm.hip); gq, gk NULL: no norm,
+// cos NULL: no rotation, pos [B][L] or NULL (the token's index); a token
+// whose position lies outside [0, n_pos) is left out.
+struct QkNormArgs {
+  Heads q, k, q_out, k_out;
+  const float *gq, *gk, *cos, *sin;
+  const int32_t* pos;
+  float eps;
+  int n_pos, B, L, H, Hkv;
+};
+hipError_t qk_norm_rope(const QkNormArgs& a, bool f32, int dh, hipStream_t s);
+
+// Rows of k, v [B][L][Hkv][dh] into (store) or out of (load) the 4-bit cache
+// (kv4.hip), positions start[b] .. start[b] + count[b] - 1 (NULL: 0, L).
+struct Kv4Rows {
+  Heads k, v;
+  void* cache;
+  const int32_t *start, *count;
+  int B, L, Hkv, L_cap;
+};
+size_t kv4_bytes(int B, int Hkv, int L_cap, int dh);
+hipError_t kv4_store(const Kv4Rows& a, int dh, hipStream_t s);
+hipError_t kv4_load(const Kv4Rows& a, int dh, hipStream_t s);
+
+// Attention of the last Lq of lens[b] cached tokens over the 4-bit cache;
+// nsplit and scale_log2 are filled in by the launch.
+struct Kv4Attn {
+  Heads q, o;
+  const void* cache;
+  const int32_t* lens;
+  float* part;
+  int B, Lq, H, Hkv, L_cap, max_len, window, sinks;
+  int nsplit;
+  float scale_log2;
+};
+size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
+hipError_t kv4_attention(Kv4Attn a, int dh, hipStream_t s);
+
 // Fixed device scratch of the decode step that allocates nothing
 // (static_scratch.hip): its size, and its address on `device` (resolved once
 // per device; `device` must be the current device the first time).

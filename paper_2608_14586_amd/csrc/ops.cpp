@@ -13,6 +13,59 @@ static_assert((int)vla::GemmOp::F32 == VLA_GEMM_F32 && (int)vla::GemmOp::RESIDUA
                   (int)vla::GemmOp::BIAS == VLA_GEMM_BIAS && (int)vla::GemmOp::GELU == VLA_GEMM_GELU &&
                   (int)vla::GemmOp::SWIGLU == VLA_GEMM_SWIGLU && (int)vla::GemmOp::QKV == VLA_GEMM_QKV,
               "vla_gemm_op names GemmOp's values");
+
+// ---- checks of the 4-bit operators' arguments
+constexpr int64_t MAX_GRID = 0x3fffffff;  // workgroups, rows of a call
+bool aligned(const void* p, uintptr_t n) { return (uintptr_t)p % n == 0; }
+bool readable(const vla_heads& h, int B, int L) {
+  return (h.p || B == 0 || L == 0) && h.seq >= 0 && h.token >= 0 && h.head >= 0;
+}
+// rows that are written must not be one and the same
+bool writable(const vla_heads& h, int B, int L, int H) {
+  return readable(h, B, L) && (B < 2 || h.seq) && (L < 2 || h.token) && (H < 2 || h.head);
+}
+bool heads_ok(const vla_heads& h) { return aligned(h.p, 16) && h.seq % 8 == 0 && h.token % 8 == 0 && h.head % 8 == 0; }
+vla::Heads heads(const vla_heads& h) { return {h.p, h.seq, h.token, h.head}; }
+
+vla_status w4_check(int N, int K, int group) {
+  if (N <= 0 || K <= 0) return VLA_ERR_INVALID_ARG;
+  if (K % 8 || (group != 32 && group != 64 && group != 128)) return VLA_ERR_UNSUPPORTED;
+  if (N > MAX_GRID || K > MAX_GRID) return VLA_ERR_UNSUPPORTED;
+  return VLA_OK;
+}
+
+vla_status kv4_check(int B, int Hkv, int L_cap, int dh) {
+  if (B < 0 || Hkv <= 0 || L_cap <= 0) return VLA_ERR_INVALID_ARG;
+  if ((dh != 64 && dh != 128) || L_cap % 32 || L_cap > 1 << 24 || (int64_t)B * Hkv > MAX_GRID)
+    return VLA_ERR_UNSUPPORTED;
+  return VLA_OK;
+}
+
+vla_status kv4_rows(const vla_heads* k, const vla_heads* v, const int32_t* start, const int32_t* count, void* cache,
+                    int B, int L, int Hkv, int L_cap, int dh, bool out, vla::Kv4Rows* a) {
+  if (!k || !v || L < 0 || B < 0 || (B && !cache)) return VLA_ERR_INVALID_ARG;
+  if (!(out ? writable(*k, B, L, Hkv) && writable(*v, B, L, Hkv) : readable(*k, B, L) && readable(*v, B, L)))
+    return VLA_ERR_INVALID_ARG;
+  const vla_status st = kv4_check(B, Hkv, L_cap, dh);
+  if (st != VLA_OK) return st;
+  if (!heads_ok(*k) || !heads_ok(*v) || !aligned(cache, 16) || !aligned(start, 4) || !aligned(count, 4) ||
+      (int64_t)B * Hkv * (L / 32 + 2) > MAX_GRID)
+    return VLA_ERR_UNSUPPORTED;
+  *a = vla::Kv4Rows{heads(*k), heads(*v), cache, start, count, B, L, Hkv, L_cap};
+  return VLA_OK;
+}
+
+// window: one that covers max_len tokens hides none, and is taken out here
+vla_status attn_check(int B, int Lq, int H, int Hkv, int dh, int max_len, int* window, int* sinks) {
+  if (B < 0 || Lq < 0 || H <= 0 || Hkv <= 0 || max_len < 0 || *window < 0 || *sinks < 0) return VLA_ERR_INVALID_ARG;
+  if (H % Hkv || (dh != 64 && dh != 128) || max_len > 1 << 24 || (int64_t)Lq * H > MAX_GRID ||
+      (int64_t)B * Lq * H > MAX_GRID)
+    return VLA_ERR_UNSUPPORTED;
+  if (*window >= max_len) *window = 0;
+  if (*sinks > max_len) *sinks = max_len;
+  if (*window == 0) *sinks = 0;
+  return VLA_OK;
+}
 }  // namespace
 
 extern "C" {
@@ -95,6 +148,101 @@ vla_status vla_op_norm_bf16(const float* x, const float* g, const float* b, floa
   hipError_t e = b ? vla::layernorm_bf16(x, g, b, eps, (bf16_t*)y, M, d, (hipStream_t)stream)
                    : vla::rmsnorm_bf16(x, g, eps, (bf16_t*)y, M, d, (hipStream_t)stream);
   return status_of(e);
+}
+
+// ------------------------------------------------- 4-bit weights and KV cache
+
+size_t vla_op_w4_packed_bytes(int N, int K, int group) {
+  return w4_check(N, K, group) == VLA_OK ? vla::w4_packed_bytes(N, K, group) : 0;
+}
+
+vla_status vla_op_w4_pack(const void* codes, const void* scales, const void* zeros, void* Wp, int N, int K, int group,
+                          void* stream) {
+  if (!codes || !scales || !Wp) return VLA_ERR_INVALID_ARG;
+  const vla_status st = w4_check(N, K, group);
+  if (st != VLA_OK) return st;
+  if (!aligned(Wp, 16) || !aligned(scales, 2) || !aligned(zeros, 2)) return VLA_ERR_UNSUPPORTED;
+  return status_of(vla::w4_pack((const uint8_t*)codes, (const bf16_t*)scales, (const bf16_t*)zeros, Wp, N, K, group,
+                                (hipStream_t)stream));
+}
+
+vla_status vla_op_gemv_w4(const void* x, int64_t ldx, const void* Wp, const float* residual, void* out, int64_t ldo,
+                          vla_dtype out_dtype, int swiglu, int M, int N, int K, int group, void* stream) {
+  if (M < 0 || ldx < 0 || ldo < 0 || (out_dtype != VLA_BF16 && out_dtype != VLA_F32) || (M && (!x || !Wp || !out)))
+    return VLA_ERR_INVALID_ARG;
+  const vla_status st = w4_check(N, K, group);
+  if (st != VLA_OK) return st;
+  if (ldx % 8 || !aligned(x, 16) || !aligned(Wp, 16) || !aligned(out, out_dtype == VLA_F32 ? 4 : 2) ||
+      !aligned(residual, 4) || (swiglu && N % 32))
+    return VLA_ERR_UNSUPPORTED;
+  if (M > 1 && (ldx < K || ldo < (swiglu ? N / 2 : N))) return VLA_ERR_INVALID_ARG;
+  if (M > 16 * 65535) return VLA_ERR_UNSUPPORTED;
+  if (M == 0) return VLA_OK;
+  return status_of(vla::gemv_w4((const bf16_t*)x, ldx, Wp, residual, out, ldo, out_dtype == VLA_F32, swiglu != 0, M, N,
+                                K, group, (hipStream_t)stream));
+}
+
+vla_status vla_op_qk_norm_rope(const vla_heads* q, const vla_heads* k, vla_dtype in_dtype, const float* gq,
+                               const float* gk, float eps, const float* cos, const float* sin, int n_pos,
+                               const int32_t* pos, const vla_heads* q_out, const vla_heads* k_out, int B, int L, int H,
+                               int Hkv, int dh, void* stream) {
+  if (!q || !k || !q_out || !k_out || !cos != !sin || n_pos < 0 || B < 0 || L < 0 || H <= 0 || Hkv <= 0 ||
+      (in_dtype != VLA_BF16 && in_dtype != VLA_F32) || !readable(*q, B, L) || !readable(*k, B, L) ||
+      !writable(*q_out, B, L, H) || !writable(*k_out, B, L, Hkv))
+    return VLA_ERR_INVALID_ARG;
+  if ((dh != 64 && dh != 128) || !heads_ok(*q) || !heads_ok(*k) || !heads_ok(*q_out) || !heads_ok(*k_out) ||
+      !aligned(gq, 16) || !aligned(gk, 16) || !aligned(cos, 16) || !aligned(sin, 16) || !aligned(pos, 4) ||
+      (int64_t)B * L > MAX_GRID || (int64_t)H + Hkv > MAX_GRID)
+    return VLA_ERR_UNSUPPORTED;
+  if (B == 0 || L == 0) return VLA_OK;
+  const vla::QkNormArgs a{heads(*q), heads(*k), heads(*q_out), heads(*k_out), gq, gk, cos, sin, pos, eps, n_pos,
+                          B, L, H, Hkv};
+  return status_of(vla::qk_norm_rope(a, in_dtype == VLA_F32, dh, (hipStream_t)stream));
+}
+
+size_t vla_op_kv4_bytes(int B, int Hkv, int L_cap, int dh) {
+  return kv4_check(B, Hkv, L_cap, dh) == VLA_OK ? vla::kv4_bytes(B, Hkv, L_cap, dh) : 0;
+}
+
+vla_status vla_op_kv4_store(const vla_heads* k, const vla_heads* v, const int32_t* start, const int32_t* count,
+                            void* cache, int B, int L, int Hkv, int L_cap, int dh, void* stream) {
+  vla::Kv4Rows a;
+  const vla_status st = kv4_rows(k, v, start, count, cache, B, L, Hkv, L_cap, dh, false, &a);
+  if (st != VLA_OK || B == 0 || L == 0) return st;
+  return status_of(vla::kv4_store(a, dh, (hipStream_t)stream));
+}
+
+vla_status vla_op_kv4_load(const void* cache, const int32_t* start, const int32_t* count, const vla_heads* k,
+                           const vla_heads* v, int B, int L, int Hkv, int L_cap, int dh, void* stream) {
+  vla::Kv4Rows a;
+  const vla_status st = kv4_rows(k, v, start, count, (void*)cache, B, L, Hkv, L_cap, dh, true, &a);
+  if (st != VLA_OK || B == 0 || L == 0) return st;
+  return status_of(vla::kv4_load(a, dh, (hipStream_t)stream));
+}
+
+size_t vla_op_attention_kv4_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks) {
+  if (attn_check(B, Lq, H, Hkv, dh, max_len, &window, &sinks) != VLA_OK || B == 0 || Lq == 0) return 0;
+  return vla::kv4_attention_scratch(B, Lq, H, Hkv, dh, max_len, window, sinks);
+}
+
+vla_status vla_op_attention_kv4(const vla_heads* q, const void* cache, const int32_t* lens, const vla_heads* o, int B,
+                                int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,
+                                void* scratch, size_t scratch_bytes, void* stream) {
+  if (!q || !o || B < 0 || Lq < 0 || !readable(*q, B, Lq) || !writable(*o, B, Lq, H) || (B && (!cache || !lens)))
+    return VLA_ERR_INVALID_ARG;
+  vla_status st = attn_check(B, Lq, H, Hkv, dh, max_len, &window, &sinks);
+  if (st == VLA_OK) st = kv4_check(B, Hkv, L_cap, dh);
+  if (st != VLA_OK) return st;
+  if (max_len > L_cap) return VLA_ERR_SHAPE;
+  if (!heads_ok(*q) || !heads_ok(*o) || !aligned(cache, 16) || !aligned(scratch, 16) || !aligned(lens, 4))
+    return VLA_ERR_UNSUPPORTED;
+  if (B == 0 || Lq == 0) return VLA_OK;
+  const size_t need = vla::kv4_attention_scratch(B, Lq, H, Hkv, dh, max_len, window, sinks);
+  if (need > scratch_bytes) return VLA_ERR_SHAPE;
+  if (need && !scratch) return VLA_ERR_INVALID_ARG;
+  const vla::Kv4Attn a{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks,
+                       1, 0.f};
+  return status_of(vla::kv4_attention(a, dh, (hipStream_t)stream));
 }
 
 }  // extern "C"
