@@ -27,6 +27,8 @@ SOURCES = ["gemm_bf16.hip", "attention_bf16.hip", "decode_bf16.hip", "norm.hip",
 # Attention keeps its score and output accumulators in VGPRs: the softmax
 # touches them every key tile, and AGPR accumulators would cost a copy each way.
 EXTRA = {"attention_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         # the results of their MFMAs are scaled right after them
+         "kv4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "w4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          # the host suffix executor: AVX-512 BF16 kernels, entered only after a CPU check
          "host_suffix.cpp": ["--offload-host-only", "-O3", "-mavx512f", "-mavx512bw", "-mavx512vl", "-mavx512bf16",
                              "-mfma"],

@@ -191,19 +191,25 @@ size_t kv4_bytes(int B, int Hkv, int L_cap, int dh);
 hipError_t kv4_store(const Kv4Rows& a, int dh, hipStream_t s);
 hipError_t kv4_load(const Kv4Rows& a, int dh, hipStream_t s);
 
+// n / d for 0 <= n < 2^31 as (n m) >> s: m = ceil(2^s / d), s = 31 + ceil(log2 d)
+struct FastDiv {
+  uint32_t m, s;
+};
 // Attention of the last Lq of lens[b] cached tokens over the 4-bit cache;
-// nsplit and scale_log2 are filled in by the launch.
+// what comes after `sinks` is filled in by the launch.
 struct Kv4Attn {
   Heads q, o;
   const void* cache;
   const int32_t* lens;
   float* part;
   int B, Lq, H, Hkv, L_cap, max_len, window, sinks;
-  int nsplit;
+  int G, chunk, nsplit;  // query heads a KV head; blocks a split; splits
+  FastDiv by_G, by_Hkv, by_rows, by_chunk;
   float scale_log2;
 };
 size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
-hipError_t kv4_attention(Kv4Attn a, int dh, hipStream_t s);
+// hipErrorOutOfMemory: a.part is smaller than kv4_attention_scratch
+hipError_t kv4_attention(Kv4Attn a, int dh, size_t scratch_bytes, hipStream_t s);
 
 // Fixed device scratch of the decode step that allocates nothing
 // (static_scratch.hip): its size, and its address on `device` (resolved once

@@ -8,34 +8,55 @@
 // bytes each, everything that attention needs of them side by side:
 //   key codes    [token 32][quarter 4][group dh/32] words: the 8 codes of dims
 //                32 group + 8 quarter + j, code j in nibble j / 2 (even j) or
-//                4 + j / 2 (odd j)
+//                4 + j / 2 (odd j), the word then rotated left by 3
 //   value codes  [quarter 4][d % 16][d / 16] words: the 8 codes of dim d of
-//                tokens 4 quarter + i (nibble i, low half) and 16 + 4 quarter + i
-//                (nibble 4 + i), i < 4
+//                tokens 4 quarter + i (nibble i) and 16 + 4 quarter + i (nibble
+//                4 + i), i < 4, the word then rotated left by 6
 //   key params   [token 32][group] words: s in the low half, m in the high
 //   value params [token 32][group] words
 // In this order a wave's loads of keys and values are contiguous and every
-// 32-bit word of codes is one lane's operand of an MFMA step.
+// 32-bit word of codes is one lane's operand of an MFMA step: nibbles i and 4 +
+// i, shifted together to the top mantissa bits of 16.0 in bf16 (keys: bits 3-6)
+// or fp16 (values: bits 6-9), make two operands 16 + c by one shift and one
+// and-or; the rotation saves the first pair its shift.
 #include "kernels.h"
 
 namespace vla {
 namespace {
 
-constexpr int BLK = 32;  // tokens per block
-constexpr uint32_t BIAS16 = 0x41804180u;  // bf16 16.0 twice
-constexpr uint32_t CODE_BITS = 0x00780078u;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// 8 codes of a word as bf16 numbers 16 + c (the code in the top four mantissa
-// bits of a bf16 with the exponent of 16)
-__device__ __forceinline__ bf16x8 unpack8(uint32_t w) {
-  const u32x4 v = {(w << 3 & CODE_BITS) | BIAS16, (w >> 1 & CODE_BITS) | BIAS16, (w >> 5 & CODE_BITS) | BIAS16,
-                   (w >> 9 & CODE_BITS) | BIAS16};
-  return __builtin_bit_cast(bf16x8, v);
-}
+constexpr int BLK = 32;  // tokens per block
+constexpr float RAISE = 8.f;  // log2 by which a weight may exceed 1
+constexpr int KROT = 3, VROT = 6;
+__host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
+
+// Words of codes to operands 16 + c.  The two constants sit in registers of
+// their own, hidden from the compiler: and-or takes no literals, and two
+// instructions in its place cost a third of the loop's unpacking.
+struct Unpack {
+  uint32_t bias, mask;
+  template <bool F16>
+  static __device__ __forceinline__ Unpack make() {
+    Unpack u{F16 ? 0x4c004c00u : 0x41804180u, F16 ? 0x03c003c0u : 0x00780078u};
+    asm("" : "+s"(u.bias), "+v"(u.mask));
+    return u;
+  }
+  __device__ __forceinline__ u32x4 operator()(uint32_t w) const {
+    return u32x4{(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
+                 (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
+  }
+};
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f32x4 mfma(const f16x8& a, const f16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
 // ------------------------------------------------------------ rows in and out
@@ -131,7 +152,7 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows a) {
       if (p)
         vs[t][j] = q.codes;
       else
-        *(uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4) = q.codes;
+        *(uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4) = rotl(q.codes, KROT);
       if (kq == 0) *(uint32_t*)(base + (p ? 36 : 32) * DH + (t * NG + g) * 4) = q.params;
     }
   }
@@ -150,8 +171,8 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows a) {
       }
     }
     if (have == 0) continue;
-    if (have != 0xffffffffu) w |= vc[i] & ~have;  // tokens of other calls keep theirs
-    vc[i] = w;
+    if (have != 0xffffffffu) w |= rotl(vc[i], 32 - VROT) & ~have;  // tokens of other calls keep theirs
+    vc[i] = rotl(w, VROT);
   }
 }
 
@@ -163,7 +184,7 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
   if (s.t0 >= s.t1) return;
   const uint8_t* base = (const uint8_t*)a.cache + (((size_t)s.b * a.Hkv + s.h) * (a.L_cap / BLK) + s.blk) * (40 * DH);
   const int tid = threadIdx.x, j = tid % LPR, g = j / 4, kq = j % 4;
-  for (int i = tid; i < 4 * DH; i += 256) vs[i] = ((const uint32_t*)(base + 16 * DH))[i];
+  for (int i = tid; i < 4 * DH; i += 256) vs[i] = rotl(((const uint32_t*)(base + 16 * DH))[i], 32 - VROT);
   __syncthreads();
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
@@ -174,7 +195,7 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
       if (t < s.t0 || t >= s.t1) continue;
       const uint32_t prm = *(const uint32_t*)(base + (p ? 36 : 32) * DH + (t * NG + g) * 4);
       const float sc = lo16(prm), mn = hi16(prm);
-      const uint32_t kw = p ? 0u : *(const uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4);
+      const uint32_t kw = p ? 0u : rotl(*(const uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4), 32 - KROT);
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -204,11 +225,14 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 //    over the groups g of 32 dims: one MFMA step a group (queries against 16
 //    keys) and two multiply-adds in fp32; sum q is a constant of the loop.
 //  * softmax: a running maximum and sum per query, in fp32, one pass.
-//  * values: with P the weights and per group P' = P s_g as hi + lo bf16 pairs
-//    (a 16-bit significand; one bf16 alone would double the error of a bf16
-//    output, since it multiplies 16 + c),
+//  * values: with P the weights and per group P' = P s_g,
 //      sum P v = sum P' (16 + c) + sum P (m_g - 16 s_g)
-//    the first sum by MFMA, the second in fp32 in the lane that holds P.
+//    the first sum by MFMA, the second in fp32 in the lane that holds P.  P' is
+//    rounded to fp16, relative to a power of two at or above the largest s_g
+//    of the group so far (`unit` is its inverse), which keeps it in fp16's
+//    range whatever the values' size: 2^-12 of at most 31 s_g P a key, a fifth of
+//    a bf16 result's own rounding.  (bf16 would be twice that rounding; hi and lo
+//    bf16 parts cost 12 instructions a row and group against 5.)
 // The 4 R queries of a tile sit in the MFMA rows 4 i + r, r < R, so with up to
 // four of them a lane holds one useful score a key and not four (R = 1).
 // P crosses from score lanes (one key each) to operand lanes (8 keys of one
@@ -221,6 +245,10 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+// a value of one lane, for all
+__device__ __forceinline__ float lane_of(float x, int lane) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane));
 }
 // over the 16 lanes of a row
 __device__ __forceinline__ float row_max(float x) {
@@ -236,82 +264,160 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + dpp<0x140>(x);
 }
 
+// over the wave
+__device__ __forceinline__ float wave_max(float x) {
+  x = row_max(x);
+  return fmaxf(fmaxf(lane_of(x, 0), lane_of(x, 16)), fmaxf(lane_of(x, 32), lane_of(x, 48)));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x = row_sum(x);
+  return (lane_of(x, 0) + lane_of(x, 16)) + (lane_of(x, 32) + lane_of(x, 48));
+}
+
 template <int N>
 struct Words {
   uint32_t w[N];
 };
+// N words at byte `at` (this lane's) + `base` (the wave's) of a buffer
 template <int N>
-__device__ __forceinline__ Words<N> load_words(const uint8_t* p) {
-  Words<N> r;
+__device__ __forceinline__ Words<N> load_words(__amdgpu_buffer_rsrc_t r, uint32_t at, uint32_t base) {
+  Words<N> x;
   if constexpr (N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-      const u32x4 v = *(const u32x4*)(p + 16 * i);
+      const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * i, base, 0));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) r.w[4 * i + e] = v[e];
+      for (int e = 0; e < 4; ++e) x.w[4 * i + e] = v[e];
     }
   } else {
-    const u32x2 v = *(const u32x2*)p;
-    r.w[0] = v[0];
-    r.w[1] = v[1];
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at, base, 0));
+    x.w[0] = v[0];
+    x.w[1] = v[1];
   }
-  return r;
+  return x;
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ int div_by(int n, const FastDiv& d) { return (int)((uint64_t)(uint32_t)n * d.m >> d.s); }
+// 1 / x of a power of two from 2^-126 to 2^126
+__device__ __forceinline__ float inverse2(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
+
+// The blocks that any of tile rows [row0, row1] of a sequence sees: `sinkb`
+// blocks of first tokens, then those from blk0 on; nb in all.
+struct Seen {
+  int pos0, pos1, blk0, sinkb, nb;
+};
+__device__ __forceinline__ Seen seen_of(const Kv4Attn& a, int len, int row0, int row1) {
+  Seen s;
+  s.pos0 = len - a.Lq + div_by(row0, a.by_G);
+  s.pos1 = len - a.Lq + div_by(row1, a.by_G);
+  const int lo = a.window ? max(s.pos0 - a.window + 1, 0) : 0;
+  s.blk0 = lo / BLK;
+  s.sinkb = min((min(a.sinks, lo) + BLK - 1) / BLK, s.blk0);
+  s.nb = s.pos1 < 0 ? 0 : s.sinkb + s.pos1 / BLK + 1 - s.blk0;
+  return s;
+}
+
+// dims d .. d + 3 of query row gr of a KV head: v / l, zeros where no key was seen
+__device__ __forceinline__ void store_row(const Kv4Attn& a, int b, int hk, int gr, int d, const f32x4& v, float l) {
+  const int q = div_by(gr, a.by_G);
+  const float f = l == 0.f ? 0.f : 1.f / l;
+  bf16_t* o = (bf16_t*)a.o.p + b * a.o.seq + q * a.o.token + (hk * a.G + gr - q * a.G) * a.o.head + d;
+  *(u32x2*)o = u32x2{pack_bf2(v[0] * f, v[1] * f), pack_bf2(v[2] * f, v[3] * f)};
 }
 
 template <int DH, int R, int W>
 __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
   constexpr int NG = DH / 32, ND = DH / 16, RT = 4 * R;
-  // P' of a wave [hi, lo][group][query][32 keys] while it runs, then its output [query][DH]
-  constexpr int PW = 2 * NG * RT * 16, OW = RT * DH;  // words
+  // P' of a wave [group][query][32 keys] while it runs, then its output [query][DH]
+  constexpr int PW = NG * RT * 16, OW = RT * DH;  // words
   __shared__ __attribute__((aligned(16))) uint32_t lds[W][PW > OW ? PW : OW];
   __shared__ float sm[W][RT], sl[W][RT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, kq = lane >> 4;
-  const int G = a.H / a.Hkv, rows = a.Lq * G, tiles = (rows + RT - 1) / RT;
-  const int split = blockIdx.x % a.nsplit, rt = blockIdx.x / a.nsplit % tiles, bh = blockIdx.x / a.nsplit / tiles;
-  const int hk = bh % a.Hkv, b = bh / a.Hkv;
+  const int bh = blockIdx.x, split = blockIdx.y;
+  const int b = div_by(bh, a.by_Hkv), hk = bh - b * a.Hkv;
+  const int G = a.G, rows = a.Lq * G, row0 = blockIdx.z * RT;
+  // queries: MFMA row c16 = 4 i + r holds tile row i R + r.  Their loads, the
+  // length's and the first block's are all on their way before any is waited for
+  u32x4 qw[NG];
+  {
+    const int row = row0 + (c16 >> 2) * R + (c16 & 3), i = div_by(row, a.by_G);
+    const bool there = (c16 & 3) < R && row < rows;
+    const bf16_t* q = (const bf16_t*)a.q.p;
+    if (there) q += b * a.q.seq + i * a.q.token + (hk * G + row - i * G) * a.q.head;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      qw[g] = u32x4{0u, 0u, 0u, 0u};
+      if (there) qw[g] = *(const u32x4*)(q + g * 32 + kq * 8);
+    }
+  }
   const int len = min(max(a.lens[b], 0), a.max_len);
-  const int row0 = rt * RT;
+  const Seen sn = seen_of(a, len, row0, min(rows, row0 + RT) - 1);
+  const int j0 = split * a.chunk, j1 = min(sn.nb, j0 + a.chunk);
+  if (j0 >= sn.nb && split) return;
 
   // this lane's rows of results: the positions of the first and last key that each sees in its window
   int last[R], first[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = row0 + kq * R + r;
-    last[r] = row < rows ? len - a.Lq + row / G : -1;
+    last[r] = row < rows ? len - a.Lq + div_by(row, a.by_G) : -1;
     first[r] = a.window ? last[r] - a.window + 1 : 0;
   }
-  // the blocks that any row of the tile sees: those of the first tokens, then the window's
-  const int pos0 = len - a.Lq + row0 / G, pos1 = len - a.Lq + (min(rows, row0 + RT) - 1) / G;
-  const int lo = a.window ? max(pos0 - a.window + 1, 0) : 0;
-  const int blk0 = lo / BLK, sinkb = min((min(a.sinks, lo) + BLK - 1) / BLK, blk0);
-  const int nb = pos1 < 0 ? 0 : sinkb + pos1 / BLK + 1 - blk0;
-  const int j0 = (int)((int64_t)split * nb / a.nsplit), j1 = (int)((int64_t)(split + 1) * nb / a.nsplit);
+  // the blocks of this sequence and head (at most 2^24 tokens: below 2^32 bytes)
+  const uint32_t bytes = (uint32_t)(a.L_cap / BLK) * (40 * DH);
+  const __amdgpu_buffer_rsrc_t cache =
+      __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.cache + (size_t)bh * bytes), (short)0, (int)bytes, 0x00020000);
+  uint32_t* pw = lds[wave];
+  const int prow = (c16 >> 2) * R + min(c16 & 3, R - 1);
+  const Unpack uk = Unpack::make<false>(), uv = Unpack::make<true>();
 
-  // queries: MFMA row c16 = 4 i + r holds tile row i R + r
-  bf16x8 qa[NG];
-  {
-    const int row = row0 + (c16 >> 2) * R + (c16 & 3);
-    const bool there = (c16 & 3) < R && row < rows;
-    const bf16_t* q = (const bf16_t*)a.q.p;
-    if (there) q += b * a.q.seq + row / G * a.q.token + (hk * G + row % G) * a.q.head;
+  Words<NG> kc[2], kp[2], vp[2];
+  Words<ND> vc;
+  auto block_of = [&](int j) { return j < sn.sinkb ? j : sn.blk0 + j - sn.sinkb; };
+  auto fetch_keys = [&](int j) {
+    const uint32_t base = (uint32_t)block_of(j) * (40 * DH);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      u32x4 v = {0u, 0u, 0u, 0u};
-      if (there) v = *(const u32x4*)(q + g * 32 + kq * 8);
-      qa[g] = __builtin_bit_cast(bf16x8, v);
+    for (int t = 0; t < 2; ++t) {
+      kc[t] = load_words<NG>(cache, t * 8 * DH + c16 * (DH / 2) + kq * (DH / 8), base);
+      kp[t] = load_words<NG>(cache, 32 * DH + (t * 16 + c16) * NG * 4, base);
     }
-  }
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  f32x4 qs[NG];  // sums of each query's groups
+  };
+  auto fetch_values = [&](int j) {
+    const uint32_t base = (uint32_t)block_of(j) * (40 * DH);
 #pragma unroll
-  for (int g = 0; g < NG; ++g)
-    qs[g] = mfma(qa[g], __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}), zero);
+    for (int t = 0; t < 2; ++t) vp[t] = load_words<NG>(cache, 36 * DH + (t * 16 + c16) * NG * 4, base);
+    vc = load_words<ND>(cache, 16 * DH + lane * ND * 4, base);
+  };
+  // the next block's keys and values are on their way as soon as this block's are used up
+  if (j0 + wave < j1) {
+    fetch_keys(j0 + wave);
+    fetch_values(j0 + wave);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+
+  bf16x8 qa[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) qa[g] = __builtin_bit_cast(bf16x8, qw[g]);
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  // the sums of each query's groups, and -16 times them: where the scores' accumulators start
+  f32x4 q16[NG];
+  float qs[NG][R];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    q16[g] = mfma(qa[g], __builtin_bit_cast(bf16x8, u32x4{0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u}), zero);
+#pragma unroll
+    for (int r = 0; r < R; ++r) qs[g][r] = -0.0625f * q16[g][r];
+  }
 
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zero;
-  float m[R], l[R], bias[R][NG];
+  float m[R], l[R], bias[R][NG], unit[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) unit[g] = 0x1p126f;  // every step but 0 exceeds it
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
@@ -319,92 +425,135 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) bias[r][g] = 0.f;
   }
-  const uint8_t* cache = (const uint8_t*)a.cache + ((size_t)b * a.Hkv + hk) * (a.L_cap / BLK) * (40 * DH);
-  uint32_t* pw = lds[wave];
-
   for (int j = j0 + wave; j < j1; j += W) {
-    const int blk = j < sinkb ? j : blk0 + j - sinkb;
-    const uint8_t* base = cache + (size_t)blk * (40 * DH);
-    Words<NG> kc[2], kp[2], vp[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      kc[t] = load_words<NG>(base + t * 8 * DH + c16 * (DH / 2) + kq * (DH / 8));
-      kp[t] = load_words<NG>(base + 32 * DH + (t * 16 + c16) * NG * 4);
-    }
-    const Words<ND> vc = load_words<ND>(base + 16 * DH + lane * ND * 4);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) vp[t] = load_words<NG>(base + 36 * DH + (t * 16 + c16) * NG * 4);
+    const int key0 = block_of(j) * BLK;
     // every row sees the whole block
-    const bool whole = blk * BLK + BLK - 1 <= pos0 && (!a.window || blk * BLK > pos1 - a.window);
-
+    const bool whole = key0 + BLK - 1 <= sn.pos0 && (!a.window || key0 > sn.pos1 - a.window);
     float p[2][R];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
+      f32x4 d[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) d[g] = mfma(qa[g], __builtin_bit_cast(bf16x8, uk(kc[t].w[g])), q16[g]);
+      // keeps the unused rows' registers from being used again before the MFMAs are done
+#pragma unroll
+      for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(d[g]));
 #pragma unroll
       for (int r = 0; r < R; ++r) p[t][r] = 0.f;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const f32x4 d = mfma(qa[g], unpack8(kc[t].w[g]), zero);
-        const float s = lo16(kp[t].w[g]), mm = fmaf(-16.f, s, hi16(kp[t].w[g]));
+      for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int r = 0; r < R; ++r) p[t][r] = fmaf(s, d[r], fmaf(mm, qs[g][r], p[t][r]));
+        for (int r = 0; r < R; ++r) p[t][r] = fmaf(hi16(kp[t].w[g]), qs[g][r], p[t][r]);
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int r = 0; r < R; ++r) p[t][r] = fmaf(lo16(kp[t].w[g]), d[g][r], p[t][r]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) p[t][r] *= a.scale_log2;
+    }
+    if (j + W < j1) fetch_keys(j + W);
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int key = key0 + t * 16 + c16;
+          // also replaces whatever the cache's unwritten rows gave
+          p[t][r] = (key <= last[r]) & ((key >= first[r]) | (key < a.sinks)) ? p[t][r] : -INFINITY;
+        }
+    }
+    float vs[2][NG], vm[2][NG], steps[2][NG];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = key0 + t * 16 + c16;
+      // what a row that nobody sees holds must not choose the unit
+      const bool seen = whole || ((key <= sn.pos1) & (!a.window | (key > sn.pos0 - a.window) | (key < a.sinks)));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const float s = lo16(vp[t].w[g]);
+        vm[t][g] = fmaf(-16.f, s, hi16(vp[t].w[g]));
+        steps[t][g] = seen ? s : 0.f;
+        vs[t][g] = steps[t][g] * unit[g];
       }
-      const int key = blk * BLK + t * 16 + c16;
+    }
+    // the running maximum moves only where a score exceeds it by RAISE, and
+    // the unit of a group's steps only where a step exceeds it, so most blocks
+    // rescale nothing
+    float up[R];
+    bool raise = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      up[r] = row_max(fmaxf(p[0][r], p[1][r]));
+      raise |= up[r] > m[r] + RAISE;
+    }
+    float most = fmaxf(vs[0][0], vs[1][0]);
+#pragma unroll
+    for (int g = 1; g < NG; ++g) most = fmaxf(most, fmaxf(vs[0][g], vs[1][g]));
+    if (__any(raise || most > 1.f)) {
+      float f[NG];  // what the group's unit changes by
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        // 1 / unit: the power of two above the largest step so far
+        const uint32_t e = __float_as_uint(row_max(fmaxf(steps[0][g], steps[1][g]))) & 0x7f800000u;
+        const float u = fminf(unit[g], e && e < 0x7f800000u ? __uint_as_float(0x7e800000u - e) : 0x1p126f);
+        f[g] = u * inverse2(unit[g]);
+        unit[g] = u;
+        vs[0][g] = steps[0][g] * u;
+        vs[1][g] = steps[1][g] * u;
+      }
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        p[t][r] *= a.scale_log2;
-        // also replaces whatever the cache's unwritten rows gave
-        if (!whole && !(key <= last[r] && (key >= first[r] || key < a.sinks))) p[t][r] = -INFINITY;
+        const float mn = fmaxf(m[r], up[r]);
+        const float al = mn == -INFINITY ? 1.f : exp2_of(m[r] - mn);
+        m[r] = mn;
+        l[r] *= al;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) bias[r][g] *= al;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d][r] *= al * f[d / 2];
       }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const float mn = fmaxf(m[r], row_max(fmaxf(p[0][r], p[1][r])));
-      const float ms = mn == -INFINITY ? 0.f : mn;
-      const float al = exp2f(m[r] - ms);
-      m[r] = mn;
-      p[0][r] = exp2f(p[0][r] - ms);
-      p[1][r] = exp2f(p[1][r] - ms);
-      l[r] = l[r] * al + (p[0][r] + p[1][r]);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) bias[r][g] *= al;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) o[d][r] *= al;
+      const float ms = m[r] == -INFINITY ? 0.f : m[r];
+      p[0][r] = exp2_of(p[0][r] - ms);
+      p[1][r] = exp2_of(p[1][r] - ms);
+      l[r] += p[0][r] + p[1][r];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of pw come first
+    __builtin_amdgcn_wave_barrier();
+    auto put = [&](int g, int r, float p0, float p1) {
+      pw[(g * RT + kq * R + r) * 16 + c16] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), f16x2));
+    };
+    if (whole) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          bias[r][g] = fmaf(p[0][r], vm[0][g], fmaf(p[1][r], vm[1][g], bias[r][g]));
+          put(g, r, p[0][r] * vs[0][g], p[1][r] * vs[1][g]);
+        }
+    } else {  // a key that the row does not see may hold NaN
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        float ps[2];
+        const bool s0 = p[0][r] != 0.f, s1 = p[1][r] != 0.f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const float s = lo16(vp[t].w[g]), mm = fmaf(-16.f, s, hi16(vp[t].w[g]));
-          // a key that the row does not see may hold NaN
-          const bool seen = whole || p[t][r] != 0.f;
-          ps[t] = seen ? p[t][r] * s : 0.f;
-          bias[r][g] = seen ? fmaf(p[t][r], mm, bias[r][g]) : bias[r][g];
+        for (int g = 0; g < NG; ++g) {
+          const float b1 = s1 ? fmaf(p[1][r], vm[1][g], bias[r][g]) : bias[r][g];
+          bias[r][g] = s0 ? fmaf(p[0][r], vm[0][g], b1) : b1;
+          put(g, r, s0 ? p[0][r] * vs[0][g] : 0.f, s1 ? p[1][r] * vs[1][g] : 0.f);
         }
-        const uint32_t hi = pack_bf2(ps[0], ps[1]);
-        const uint32_t rest = pack_bf2(ps[0] - lo16(hi), ps[1] - hi16(hi));
-        pw[(g * RT + kq * R + r) * 16 + c16] = hi;
-        pw[((NG + g) * RT + kq * R + r) * 16 + c16] = rest;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int prow = (c16 >> 2) * R + min(c16 & 3, R - 1);
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const bf16x8 ph = __builtin_bit_cast(bf16x8, *(const u32x4*)&pw[(g * RT + prow) * 16 + kq * 4]);
-      const bf16x8 pl = __builtin_bit_cast(bf16x8, *(const u32x4*)&pw[((NG + g) * RT + prow) * 16 + kq * 4]);
-#pragma unroll
-      for (int d = 2 * g; d < 2 * g + 2; ++d) {
-        const bf16x8 v = unpack8(vc.w[d]);
-        o[d] = mfma(ph, v, o[d]);
-        o[d] = mfma(pl, v, o[d]);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const f16x8 ph = __builtin_bit_cast(f16x8, *(const u32x4*)&pw[(g * RT + prow) * 16 + kq * 4]);
+#pragma unroll
+      for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] = mfma(ph, __builtin_bit_cast(f16x8, uv(vc.w[d])), o[d]);
+    }
+    if (j + W < j1) fetch_values(j + W);
   }
 
   // join the waves: lane (c16, kq) holds dims 16 d + c16 of tile rows kq R + r
@@ -420,64 +569,111 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float bs = row_sum(bias[r][g]);
+      const float bs = row_sum(bias[r][g]), w = inverse2(unit[g]);
 #pragma unroll
-      for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = o[d][r] + bs;
+      for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = fmaf(o[d][r], w, bs);
     }
   }
   __syncthreads();
-  for (int i = tid; i < RT * DH; i += W * 64) {
-    const int row = i / DH, d = i % DH;
-    if (row0 + row >= rows) break;
-    float mx = -INFINITY;
+  for (int i = tid; i < RT * DH / 4; i += W * 64) {
+    const int row = i / (DH / 4), d = i % (DH / 4) * 4, gr = row0 + row;
+    if (gr >= rows) break;
+    float mx = sm[0][row];
 #pragma unroll
-    for (int w = 0; w < W; ++w) mx = fmaxf(mx, sm[w][row]);
-    float ls = 0.f, v = 0.f;
+    for (int w = 1; w < W; ++w) mx = fmaxf(mx, sm[w][row]);
+    float ls = 0.f;
+    f32x4 v = zero;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float f = sm[w][row] == -INFINITY ? 0.f : exp2f(sm[w][row] - mx);
+      const float f = sm[w][row] == -INFINITY ? 0.f : exp2_of(sm[w][row] - mx);
       ls = fmaf(f, sl[w][row], ls);
-      v = fmaf(f, ((const float*)lds[w])[i], v);
+      const f32x4 x = *(const f32x4*)((const float*)lds[w] + row * DH + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(f, x[e], v[e]);
     }
-    if (a.nsplit == 1) {
-      const int gr = row0 + row;
-      ((bf16_t*)a.o.p)[b * a.o.seq + gr / G * a.o.token + (hk * G + gr % G) * a.o.head + d] =
-          f2bf(ls == 0.f ? 0.f : v / ls);
+    if (sn.nb <= a.chunk) {
+      store_row(a, b, hk, gr, d, v, ls);
     } else {
-      float* part = a.part + (((size_t)bh * rows + row0 + row) * a.nsplit + split) * (DH + 2);
-      part[2 + d] = v;
-      if (d == 0) {
-        part[0] = mx;
-        part[1] = ls;
+      const size_t at = ((size_t)bh * rows + gr) * a.nsplit + split;
+      *(f32x4*)(a.part + at * DH + d) = v;
+      if (d == 0) *(f32x2*)(a.part + (size_t)gridDim.x * rows * a.nsplit * DH + at * 2) = f32x2{mx, ls};
+    }
+  }
+}
+
+// Joins the splits of a query row where there is more than one; one wave a
+// row.  Lane s takes the maximum and sum of split s, so that the weights of 64
+// splits cost one load and one reduction; the outputs of CB splits are in
+// flight together, the first ones beside the length's load.
+template <int DH, int R>
+__global__ __launch_bounds__(64) void kv4_combine_kernel(Kv4Attn a, int total) {
+  constexpr int CB = 16, RT = 4 * R, D = DH / 64;  // dims a lane
+  typedef float vec __attribute__((ext_vector_type(D)));
+  const int rows = a.Lq * a.G, row = blockIdx.x, lane = threadIdx.x;
+  const int bh = div_by(row, a.by_rows), gr = row - bh * rows;
+  const int b = div_by(bh, a.by_Hkv), hk = bh - b * a.Hkv;
+  const float* part = a.part + (size_t)row * a.nsplit * DH + lane * D;
+  const f32x2* ml = (const f32x2*)(a.part + (size_t)total * a.nsplit * DH) + (size_t)row * a.nsplit;
+  vec os[CB];
+  auto load = [&](int s0, int n) {
+#pragma unroll
+    for (int s = 0; s < CB; ++s) os[s] = *(const vec*)(part + (size_t)min(s0 + s, n - 1) * DH);
+  };
+  f32x2 x = ml[min(lane, a.nsplit - 1)];
+  load(0, a.nsplit);  // what was not written is not used
+  const int length = a.lens[b];
+  __builtin_amdgcn_sched_barrier(0);
+  const int row0 = gr / RT * RT;
+  const Seen sn = seen_of(a, min(max(length, 0), a.max_len), row0, min(rows, row0 + RT) - 1);
+  const int ns = div_by(sn.nb + a.chunk - 1, a.by_chunk);
+  float mx = -INFINITY, l = 0.f;
+  vec v = {};
+  for (int s0 = 0; s0 < ns; s0 += 64) {
+    if (s0) x = ml[min(s0 + lane, ns - 1)];
+    const float m = s0 + lane < ns ? x[0] : -INFINITY, mn = fmaxf(mx, wave_max(m));
+    const float f0 = mx == -INFINITY ? 0.f : exp2_of(mx - mn);
+    const float f = m == -INFINITY ? 0.f : exp2_of(m - mn);
+    l = fmaf(l, f0, wave_sum(m == -INFINITY ? 0.f : f * x[1]));
+    v *= f0;
+    mx = mn;
+    const int n = min(64, ns - s0);
+    for (int s1 = 0; s1 < n; s1 += CB) {
+      if (s0 + s1) load(s0 + s1, ns);
+#pragma unroll
+      for (int s = 0; s < CB; ++s) {
+        const float w = lane_of(f, s1 + s);
+        if (s1 + s < n) v += w * os[s];
       }
     }
   }
+  if (ns < 2) return;  // written by the one split
+  const int q = div_by(gr, a.by_G);
+  const float f = l == 0.f ? 0.f : 1.f / l;
+  bf16_t* o = (bf16_t*)a.o.p + b * a.o.seq + q * a.o.token + (hk * a.G + gr - q * a.G) * a.o.head + lane * D;
+  if constexpr (D == 2)
+    *(uint32_t*)o = pack_bf2(v[0] * f, v[1] * f);
+  else
+    *o = f2bf(v[0] * f);
 }
 
-// joins the splits of one query row (blockIdx.x), one thread a dim
-template <int DH>
-__global__ __launch_bounds__(DH) void kv4_combine_kernel(Kv4Attn a) {
-  const int G = a.H / a.Hkv, rows = a.Lq * G;
-  const int gr = blockIdx.x % rows, bh = blockIdx.x / rows, hk = bh % a.Hkv, b = bh / a.Hkv, d = threadIdx.x;
-  const float* part = a.part + (size_t)blockIdx.x * a.nsplit * (DH + 2);
-  float mx = -INFINITY;
-  for (int s = 0; s < a.nsplit; ++s) mx = fmaxf(mx, part[s * (DH + 2)]);
-  float l = 0.f, v = 0.f;
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float* p = part + s * (DH + 2);
-    const float f = p[0] == -INFINITY ? 0.f : exp2f(p[0] - mx);
-    l = fmaf(f, p[1], l);
-    v = fmaf(f, p[2 + d], v);
-  }
-  ((bf16_t*)a.o.p)[b * a.o.seq + gr / G * a.o.token + (hk * G + gr % G) * a.o.head + d] = f2bf(l == 0.f ? 0.f : v / l);
+FastDiv fast_div(uint32_t d) {
+  uint32_t s = 31;
+  while ((1ull << (s - 31)) < d) ++s;
+  return {(uint32_t)(((1ull << s) + d - 1) / d), s};
 }
-
-constexpr int W_ATT = 4;
 
 struct Plan {
-  int R, tiles, nsplit;
+  int R, W, tiles, chunk, nsplit;
 };
-// Splits over the keys: enough workgroups for two a CU, as long as every wave has a block of its own.
+// Waves a workgroup and blocks a wave, by the estimated time of each choice,
+// in tenths of a microsecond: a wave alone on its SIMD takes 1.8 a block, a
+// SIMD 0.8 a block and 0.8 more a wave, whatever R and dh (memory latency and
+// the LDS round trip weigh more than instructions); one CU takes the
+// workgroups past 256; joining splits costs 5, and 0.5 more past every 16
+// splits.  Over 31 calls timed at every choice (1 to 64 sequences, 1 to 131072
+// tokens, R = 1, 2, 4, windows), 17 choices each, what this takes is 0.06%
+// slower than the fastest on average and 1% at most; a fixed aim of 1024
+// workgroups of four waves lost up to 40%.
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
   Plan p;
@@ -488,30 +684,37 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
     const int64_t w = ((int64_t)window + Lq - 1 + BLK - 1) / BLK + 1 + cdiv(sinks, BLK);
     if (w < blocks) blocks = w;
   }
-  const int64_t wgs = (int64_t)B * Hkv * p.tiles;
-  int64_t ns = (512 + wgs - 1) / wgs;
-  const int64_t most = (blocks + W_ATT - 1) / W_ATT;
-  if (ns > most) ns = most;
-  p.nsplit = ns < 1 ? 1 : (int)ns;
+  if (blocks < 1) blocks = 1;
+  const int64_t bt = (int64_t)B * Hkv * p.tiles;
+  int64_t best = INT64_MAX;
+  for (int W = 4; W <= 8; W += 4) {
+    const int64_t most = (blocks + W - 1) / W;
+    for (int64_t per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
+      if (per > most) per = most;
+      const int64_t ns = (blocks + per * W - 1) / (per * W);
+      const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 18 * per, simd = a_simd * (8 * per + 8);
+      const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 50 + 5 * ((ns - 1) / 16) : 0);
+      if (cost < best && ns <= 4096) best = cost, p.W = W, p.chunk = (int)(per * W), p.nsplit = (int)ns;
+      if (per == most) break;
+    }
+  }
   return p;
 }
 
-template <int DH, int R>
+template <int DH, int R, int W>
 hipError_t launch_attention(const Kv4Attn& a, int tiles, hipStream_t s) {
-  const int64_t grid = (int64_t)a.B * a.Hkv * tiles * a.nsplit;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((kv4_attention_kernel<DH, R, W_ATT>), dim3((unsigned)grid), dim3(W_ATT * 64), 0, s, a);
+  hipLaunchKernelGGL((kv4_attention_kernel<DH, R, W>), dim3(a.B * a.Hkv, a.nsplit, tiles), dim3(W * 64), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
-  hipLaunchKernelGGL((kv4_combine_kernel<DH>), dim3((unsigned)(a.B * a.H * a.Lq)), dim3(DH), 0, s, a);
+  hipLaunchKernelGGL((kv4_combine_kernel<DH, R>), dim3(a.B * a.Lq * a.H), dim3(64), 0, s, a, a.B * a.Lq * a.H);
   return hipGetLastError();
 }
-template <int DH>
+template <int DH, int W>
 hipError_t by_rows(const Kv4Attn& a, const Plan& p, hipStream_t s) {
   switch (p.R) {
-    case 1: return launch_attention<DH, 1>(a, p.tiles, s);
-    case 2: return launch_attention<DH, 2>(a, p.tiles, s);
-    default: return launch_attention<DH, 4>(a, p.tiles, s);
+    case 1: return launch_attention<DH, 1, W>(a, p.tiles, s);
+    case 2: return launch_attention<DH, 2, W>(a, p.tiles, s);
+    default: return launch_attention<DH, 4, W>(a, p.tiles, s);
   }
 }
 
@@ -537,16 +740,30 @@ hipError_t kv4_load(const Kv4Rows& a, int dh, hipStream_t s) {
   return hipGetLastError();
 }
 
-size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks) {
-  const Plan p = plan_of(B, Lq, H, Hkv, max_len, window, sinks);
+namespace {
+size_t scratch_of(const Plan& p, int B, int Lq, int H, int dh) {
   return p.nsplit == 1 ? 0 : (size_t)B * Lq * H * p.nsplit * (dh + 2) * sizeof(float);
 }
+}  // namespace
 
-hipError_t kv4_attention(Kv4Attn a, int dh, hipStream_t s) {
+size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks) {
+  return scratch_of(plan_of(B, Lq, H, Hkv, max_len, window, sinks), B, Lq, H, dh);
+}
+
+hipError_t kv4_attention(Kv4Attn a, int dh, size_t scratch_bytes, hipStream_t s) {
   const Plan p = plan_of(a.B, a.Lq, a.H, a.Hkv, a.max_len, a.window, a.sinks);
+  if (p.tiles > 65535) return hipErrorInvalidValue;
+  if (scratch_of(p, a.B, a.Lq, a.H, dh) > scratch_bytes) return hipErrorOutOfMemory;
+  a.G = a.H / a.Hkv;
+  a.by_G = fast_div(a.G);
+  a.by_Hkv = fast_div(a.Hkv);
+  a.by_chunk = fast_div(p.chunk);
+  a.by_rows = fast_div(a.Lq * a.G);
+  a.chunk = p.chunk;
   a.nsplit = p.nsplit;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
-  return dh == 128 ? by_rows<128>(a, p, s) : by_rows<64>(a, p, s);
+  if (p.W == 8) return dh == 128 ? by_rows<128, 8>(a, p, s) : by_rows<64, 8>(a, p, s);
+  return dh == 128 ? by_rows<128, 4>(a, p, s) : by_rows<64, 4>(a, p, s);
 }
 
 }  // namespace vla

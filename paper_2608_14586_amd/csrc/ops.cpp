@@ -237,12 +237,10 @@ vla_status vla_op_attention_kv4(const vla_heads* q, const void* cache, const int
   if (!heads_ok(*q) || !heads_ok(*o) || !aligned(cache, 16) || !aligned(scratch, 16) || !aligned(lens, 4))
     return VLA_ERR_UNSUPPORTED;
   if (B == 0 || Lq == 0) return VLA_OK;
-  const size_t need = vla::kv4_attention_scratch(B, Lq, H, Hkv, dh, max_len, window, sinks);
-  if (need > scratch_bytes) return VLA_ERR_SHAPE;
-  if (need && !scratch) return VLA_ERR_INVALID_ARG;
-  const vla::Kv4Attn a{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks,
-                       1, 0.f};
-  return status_of(vla::kv4_attention(a, dh, (hipStream_t)stream));
+  if (!scratch && scratch_bytes) return VLA_ERR_INVALID_ARG;
+  const vla::Kv4Attn a{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks};
+  const hipError_t e = vla::kv4_attention(a, dh, scratch_bytes, (hipStream_t)stream);
+  return e == hipErrorOutOfMemory ? VLA_ERR_SHAPE : status_of(e);
 }
 
 }  // extern "C"

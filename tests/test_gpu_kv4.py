@@ -209,6 +209,49 @@ def test_attention_keeps_hidden_rows_out():
     assert np.isnan(b[0, 3]).all()
 
 
+@pytest.mark.parametrize("byte", [0x7e, 0x01, 0x80, 0xc3])
+def test_attention_beside_unwritten_rows(byte):
+    """The block that holds a sequence's last tokens also holds rows that were
+    never written; whatever numbers they look like (steps of 8e37 or 2e-38,
+    negative ones), the result is that of a clean cache, to the last bit."""
+    from paper_2608_14586_amd import binding as vb
+    B, Lq, H, Hkv, dh = 2, 2, 8, 2, 64
+    lens = [37, 3]
+    k, v = _kv(("beside",), B, 37, Hkv, dh)
+    q = ref.to_dev(ref.normal(("bsq",), (B, Lq, H, dh)))
+    out = []
+    for fill in (0, byte):
+        cache = _cache(B, Hkv, 64, dh, fill)
+        vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(v), None, _i32(*lens), cache, 64)
+        out.append(_attend(q, cache, 64, Hkv, lens, 37))
+    assert np.array_equal(out[0], out[1])
+    _check(out[1], ref.from_dev(q), k, v, lens, 0, 0)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 30, 2.0 ** 100])
+def test_attention_at_any_size_of_values(scale):
+    """Values far from one, and groups whose steps differ by 2^60 or are zero
+    in their first tokens: every group's result is as exact as its own values'
+    size allows."""
+    from paper_2608_14586_amd import binding as vb
+    B, H, Hkv, dh, n = 1, 4, 2, 128, 200
+    k, v = _kv(("sizes",), B, n, Hkv, dh)
+    v *= scale
+    v[..., 32:64] *= 2.0 ** -40
+    v[:, :70, :, 64:96] = scale  # constant at first
+    v[:, :, :, 96:] = np.where(np.arange(n)[:, None, None] < 100, 2.0 ** -30, 1.0) * v[:, :, :, 96:]
+    q = ref.normal(("szq",), (B, 1, H, dh))
+    cache = _cache(B, Hkv, 224, dh)
+    vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(v), None, None, cache, 224)
+    got = _attend(ref.to_dev(q), cache, 224, Hkv, [n], n)
+    for g in range(4):  # each group against its own size
+        at = slice(32 * g, 32 * g + 32)
+        kc, vc = ref.cached(k), ref.cached(v)
+        want, mag = ref.attention(q[0], kc[0], vc[0], n, 0, 0)
+        top = np.abs(vc[0, ..., at]).max()
+        assert (np.abs(got[0] - want)[..., at] <= 2.0 ** -8 * np.abs(want[..., at]) + 2.0 ** -11 * (mag[..., at] + top)).all(), g
+
+
 def test_attention_lens_are_cut():
     """Lengths below 0 count as 0 and above max_len as max_len."""
     from paper_2608_14586_amd import binding as vb
