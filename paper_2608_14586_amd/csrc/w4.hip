@@ -28,21 +28,30 @@ namespace {
 // The packed weights: rows in tiles of 16, k in blocks of 128.
 //   codes  [tile][block][lane 64][4] 32-bit words: lane l holds row l % 16; its
 //          word t the 8 codes k = 32 t + 8 (l / 16) + j of the block, code j
-//          in nibble j / 2 (even j) or 4 + j / 2 (odd j)
+//          in nibble j / 2 (even j) or 4 + j / 2 (odd j), the word rotated
+//          left by 3: nibbles i and 4 + i, 4 i bits to the right, are then the
+//          top mantissa bits of a pair
 //   params [tile][block][row 16][128 / g] 32-bit words: scale in the low,
 //          zero point in the high half
 // Rows past N and inputs past K have code 0 and scale 0.
 __host__ __device__ inline size_t code_bytes(int N, int K) { return (size_t)cdiv(N, 16) * cdiv(K, 128) * 1024; }
 
-constexpr uint32_t BIAS16 = 0x41804180u;  // bf16 16.0 twice
-constexpr uint32_t CODE_BITS = 0x00780078u;
+constexpr int ROT = 3;
+__host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
 
-// 8 codes of a word as bf16 numbers 16 + c
-__device__ __forceinline__ bf16x8 unpack8(uint32_t w) {
-  const u32x4 v = {(w << 3 & CODE_BITS) | BIAS16, (w >> 1 & CODE_BITS) | BIAS16, (w >> 5 & CODE_BITS) | BIAS16,
-                   (w >> 9 & CODE_BITS) | BIAS16};
-  return __builtin_bit_cast(bf16x8, v);
-}
+// 8 codes of a word as bf16 numbers 16 + c.  The two constants sit in registers
+// of their own, hidden from the compiler: and-or takes no literals, and two
+// instructions in its place cost a third of the loop's unpacking.
+struct Unpack {
+  uint32_t bias = 0x41804180u, mask = 0x00780078u;
+  __device__ __forceinline__ Unpack() { asm("" : "+s"(bias), "+v"(mask)); }
+  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
+    const u32x4 v = {(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
+                     (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias,
+                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
+    return __builtin_bit_cast(bf16x8, v);
+  }
+};
 
 __device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -56,33 +65,41 @@ struct W4Args {
   void* out;
   int64_t ldo;
   int M, N, K;
+  bool f32;
+};
+
+template <int N>
+struct alignas(4 * N) Params {
+  uint32_t w[N];
 };
 
 // One workgroup: NT tiles of 16 weight rows (SWIGLU: NT / 2 gate tiles and
 // the up tiles of the same features), 16 rows of x; its W waves take every
 // W-th block of 128 k and join their sums in LDS.
-template <int NT, int R, int GPB, int W, bool SWIGLU, bool F32>
+template <int NT, int R, int GPB, int W, bool SWIGLU>
 __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
-  __shared__ float red[W][NT * R][64];
+  // a wave's block of x, then its sums
+  constexpr int XW = 4 * R * 16, SW = NT * R * 16;  // 16-byte words
+  __shared__ u32x4 lds[W][XW > SW ? XW : SW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, kq = lane >> 4;
   const int ntiles = cdiv(a.N, 16), KB = cdiv(a.K, 128);
   constexpr int TW = SWIGLU ? NT / 2 : NT;  // output tiles
   const int t0 = blockIdx.x * TW;
   const int m0 = blockIdx.y * 16;
-  int tile[NT];
+  const uint8_t* codes[NT];
+  const uint32_t* params[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int t = SWIGLU ? (i < TW ? min(t0 + i, ntiles / 2 - 1) : ntiles / 2 + min(t0 + i - TW, ntiles / 2 - 1))
                          : min(t0 + i, ntiles - 1);
-    tile[i] = t;
+    codes[i] = a.wp + (size_t)t * KB * 1024;
+    params[i] = (const uint32_t*)(a.wp + code_bytes(a.N, a.K)) + (size_t)t * KB * 16 * GPB;
   }
-  // x rows: MFMA row c16 = 4 i + r holds row i R + r (r < R); others and rows
-  // past M read as zero
-  const int m = (c16 >> 2) * R + (c16 & 3);
-  const bool row_there = (c16 & 3) < R && m0 + m < a.M;
-  const bf16_t* xrow = a.x + (size_t)(row_there ? m0 + m : 0) * a.ldx;
-  const uint8_t* pp = a.wp + code_bytes(a.N, a.K);
+  const int mrows = min(a.M - m0, 16);
+  const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(
+      (void*)(a.x + (size_t)m0 * a.ldx), (short)0, (int)(((size_t)(mrows - 1) * a.ldx + a.K) * 2), 0x00020000);
+  const Unpack unpack;
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
   float y[NT][R];
 #pragma unroll
@@ -90,63 +107,115 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
 #pragma unroll
     for (int r = 0; r < R; ++r) y[i][r] = 0.f;
 
-  for (int kb = wave; kb < KB; kb += W) {
-    u32x4 cw[NT];
-    uint32_t pw[NT][GPB];
-    bf16x8 xa[4];
+  // x: load q covers rows 4 q .. 4 q + 3, 16 lanes and 256 bytes each (a lane
+  // per operand word would touch 16 rows in 16-byte pieces, and the gather cost
+  // more than the weights at 16 rows); rows and inputs that are not there lie
+  // outside the buffer and read as zero.  LDS turns them into operands: MFMA row
+  // 4 i + r is row i R + r (r < R; the others repeat one, their results are not
+  // used); word c of row m lies at c ^ 4 (m & 3), free of bank conflicts.
+  // whether the next block's x is asked for before the products or after them:
+  // before, except at 16 rows, whose 16 registers are better asked for last (9.5 -> 8.8 us
+  // at 13 rows, N = 4096, K = 11008; 7.2 -> 6.5 the other way at one row)
+  constexpr bool EARLY_X = R != 4;
+  u32x4* xs = lds[wave];
+  uint32_t xat[R];
+#pragma unroll
+  for (int q = 0; q < R; ++q) {
+    const int row = 4 * q + kq;
+    xat[q] = row < mrows ? (uint32_t)(row * a.ldx * 2) + c16 * 16 : 0x80000000u;
+  }
+  const int xput = kq * 16 + (c16 ^ kq * 4);
+  const int xrow = (c16 >> 2) * R + min(c16 & 3, R - 1), xget = xrow * 16, xswz = (xrow & 3) * 4;
+
+  u32x4 cw[NT], xw[R];
+  Params<GPB> pw[NT];
+  auto load_x = [&](int kb) {
+    const bool in = kb * 128 + c16 * 8 < a.K;
+#pragma unroll
+    for (int q = 0; q < R; ++q)
+      xw[q] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, in ? xat[q] + kb * 256 : 0x80000000u, 0, 0));
+  };
+  auto load_w = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      cw[i] = *(const u32x4*)(a.wp + ((size_t)tile[i] * KB + kb) * 1024 + lane * 16);
-      const uint32_t* p = (const uint32_t*)pp + (((size_t)tile[i] * KB + kb) * 16 + c16) * GPB;
-#pragma unroll
-      for (int g = 0; g < GPB; ++g) pw[i][g] = p[g];
+      cw[i] = *(const u32x4*)(codes[i] + (size_t)kb * 1024 + lane * 16);
+      pw[i] = ((const Params<GPB>*)params[i])[kb * 16 + c16];
     }
+  };
+  // a block's registers are loaded again as soon as they are used up
+  if (wave < KB) {
+    load_w(wave);
+    load_x(wave);
+  }
+  for (int kb = wave; kb < KB; kb += W) {
+    const bool more = kb + W < KB;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int k = kb * 128 + t * 32 + kq * 8;
-      u32x4 v = {0u, 0u, 0u, 0u};
-      if (row_there && k < a.K) v = *(const u32x4*)(xrow + k);
-      xa[t] = __builtin_bit_cast(bf16x8, v);
-    }
+    for (int q = 0; q < R; ++q) xs[q * 64 + xput] = xw[q];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    bf16x8 xa[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) xa[t] = __builtin_bit_cast(bf16x8, xs[xget + ((t * 4 + kq) ^ xswz)]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (EARLY_X && more) load_x(kb + W);
+    f32x4 sum[GPB], d[GPB][NT];
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
-      f32x4 xs = {0.f, 0.f, 0.f, 0.f}, d[NT];
+      sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NT; ++i) d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < NT; ++i) d[g][i] = sum[g];
 #pragma unroll
       for (int t = g * 4 / GPB; t < (g + 1) * 4 / GPB; ++t) {
-        xs = mfma(xa[t], ones, xs);
+        sum[g] = mfma(xa[t], ones, sum[g]);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) d[i] = mfma(xa[t], unpack8(cw[i][t]), d[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const float s = __uint_as_float(pw[i][g] << 16), z = __uint_as_float(pw[i][g] & 0xffff0000u);
-#pragma unroll
-        for (int r = 0; r < R; ++r) y[i][r] = fmaf(s, fmaf(-16.f - z, xs[r], d[i][r]), y[i][r]);
+        for (int i = 0; i < NT; ++i) d[g][i] = mfma(xa[t], unpack(cw[i][t]), d[g][i]);
       }
     }
+    // keeps the unused rows' registers from being used again before the MFMAs are done
+#pragma unroll
+    for (int g = 0; g < GPB; ++g) {
+      asm volatile("" : "+v"(sum[g]));
+#pragma unroll
+      for (int i = 0; i < NT; ++i) asm volatile("" : "+v"(d[g][i]));
+    }
+    Params<GPB> pv[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) pv[i] = pw[i];
+    if (more) load_w(kb + W);
+    if (!EARLY_X && more) load_x(kb + W);
+#pragma unroll
+    for (int g = 0; g < GPB; ++g)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const uint32_t p = pv[i].w[g];
+        const float s = __uint_as_float(p << 16), z = __uint_as_float(p & 0xffff0000u);
+#pragma unroll
+        for (int r = 0; r < R; ++r) y[i][r] = fmaf(s, fmaf(-16.f - z, sum[g][r], d[g][i][r]), y[i][r]);
+      }
   }
+  float* red = (float*)lds[wave];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int r = 0; r < R; ++r) red[wave][i * R + r][lane] = y[i][r];
+    for (int r = 0; r < R; ++r) red[(i * R + r) * 64 + lane] = y[i][r];
   __syncthreads();
   for (int e = wave; e < TW * R; e += W) {
     const int i = e / R, r = e % R;
     float v = 0.f, u = 0.f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) v += red[w][e][lane];
+    for (int w = 0; w < W; ++w) v += ((const float*)lds[w])[e * 64 + lane];
     if constexpr (SWIGLU) {
 #pragma unroll
-      for (int w = 0; w < W; ++w) u += red[w][TW * R + e][lane];
+      for (int w = 0; w < W; ++w) u += ((const float*)lds[w])[(TW * R + e) * 64 + lane];
     }
     const int n = (t0 + i) * 16 + c16, row = m0 + kq * R + r;
     if (n < (SWIGLU ? a.N / 2 : a.N) && row < a.M) {
       if constexpr (SWIGLU) v = v / (1.f + __expf(-v)) * u;
       const size_t at = (size_t)row * a.ldo + n;
       if (a.res) v += a.res[at];
-      if constexpr (F32)
+      if (a.f32)
         ((float*)a.out)[at] = v;
       else
         ((bf16_t*)a.out)[at] = f2bf(v);
@@ -154,24 +223,23 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
   }
 }
 
-template <int NT, int R, int W, bool SWIGLU, bool F32>
+template <int NT, int R, int W, bool SWIGLU>
 hipError_t launch(const W4Args& a, int group, hipStream_t s) {
   const int tiles = SWIGLU ? a.N / 32 : cdiv(a.N, 16), tw = SWIGLU ? NT / 2 : NT;
   const dim3 grid(cdiv(tiles, tw), cdiv(a.M, 16)), block(W * 64);
   switch (group) {
-    case 32: hipLaunchKernelGGL((w4_kernel<NT, R, 4, W, SWIGLU, F32>), grid, block, 0, s, a); break;
-    case 64: hipLaunchKernelGGL((w4_kernel<NT, R, 2, W, SWIGLU, F32>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((w4_kernel<NT, R, 1, W, SWIGLU, F32>), grid, block, 0, s, a); break;
+    case 32: hipLaunchKernelGGL((w4_kernel<NT, R, 4, W, SWIGLU>), grid, block, 0, s, a); break;
+    case 64: hipLaunchKernelGGL((w4_kernel<NT, R, 2, W, SWIGLU>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((w4_kernel<NT, R, 1, W, SWIGLU>), grid, block, 0, s, a); break;
   }
   return hipGetLastError();
 }
 
-template <bool SWIGLU, bool F32>
+template <int NT, int W, bool SWIGLU>
 hipError_t by_rows(const W4Args& a, int group, hipStream_t s) {
-  constexpr int NT = SWIGLU ? 2 : 1;
-  if (a.M <= 4) return launch<NT, 1, 8, SWIGLU, F32>(a, group, s);
-  if (a.M <= 8) return launch<NT, 2, 8, SWIGLU, F32>(a, group, s);
-  return launch<NT, 4, 8, SWIGLU, F32>(a, group, s);
+  if (a.M <= 4) return launch<NT, 1, W, SWIGLU>(a, group, s);
+  if (a.M <= 8) return launch<NT, 2, W, SWIGLU>(a, group, s);
+  return launch<NT, 4, W, SWIGLU>(a, group, s);
 }
 
 // one thread per word of the packed weights
@@ -200,7 +268,7 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict_
         w = scales[(size_t)n * G + gg] | z << 16;
       }
     }
-    wp[i] = w;
+    wp[i] = i < nc ? rotl(w, ROT) : w;
   }
 }
 
@@ -220,9 +288,20 @@ hipError_t w4_pack(const uint8_t* codes, const bf16_t* scales, const bf16_t* zer
 
 hipError_t gemv_w4(const bf16_t* x, int64_t ldx, const void* wp, const float* res, void* out, int64_t ldo, bool f32,
                    bool swiglu, int M, int N, int K, int group, hipStream_t s) {
-  const W4Args a{x, ldx, (const uint8_t*)wp, res, out, ldo, M, N, K};
-  if (swiglu) return f32 ? by_rows<true, true>(a, group, s) : by_rows<true, false>(a, group, s);
-  return f32 ? by_rows<false, true>(a, group, s) : by_rows<false, false>(a, group, s);
+  const W4Args a{x, ldx, (const uint8_t*)wp, res, out, ldo, M, N, K, f32};
+  // Waves a workgroup: the more there are, the shorter each one's chain of
+  // loads.  With two workgroups a CU or more other workgroups fill the waits
+  // instead, and short chains have none; there four waves do where a block is
+  // much work (16 rows, two tiles).  us at 4, 8, 16 waves: N = 4096, K = 11008,
+  // one row 13.7, 8.4, 6.5; N = 12288, K = 4096, one row 7.3, 6.8, 7.2, 16 rows
+  // 9.1, 9.3, 11.1; N = 3830, K = 1184, four rows 3.2, 3.0, 3.2.
+  const int tiles = swiglu ? N / 32 : cdiv(N, 16);
+  const int64_t wgs = (int64_t)tiles * cdiv(M, 16);
+  if (wgs < 512 && K > 2944)
+    return swiglu ? by_rows<2, 16, true>(a, group, s) : by_rows<1, 16, false>(a, group, s);
+  if (wgs < 512 || (M <= 8 && !swiglu))
+    return swiglu ? by_rows<2, 8, true>(a, group, s) : by_rows<1, 8, false>(a, group, s);
+  return swiglu ? by_rows<2, 4, true>(a, group, s) : by_rows<1, 4, false>(a, group, s);
 }
 
 }  // namespace vla
