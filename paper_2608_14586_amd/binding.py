@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, c_char_p, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 import numpy as np
@@ -54,10 +55,6 @@ class vla_block_weights(ctypes.Structure):
 class vla_boundary(ctypes.Structure):
     _fields_ = [("hidden", c_void_p), ("hidden_bytes", c_size_t), ("kv", c_void_p), ("kv_bytes", c_size_t),
                 ("out_dtype", c_int), ("frame_id", c_uint64)]
-
-
-class vla_heads(ctypes.Structure):
-    _fields_ = [("p", c_void_p), ("seq", c_int64), ("token", c_int64), ("head", c_int64)]
 
 
 class vla_vision_cfg(ctypes.Structure):
@@ -120,15 +117,15 @@ def lib():
             "vla_op_w4_pack": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
             "vla_op_gemv_w4": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int, c_int,
                                c_int, c_int, c_void_p],
-            "vla_op_qk_norm_rope": [P(vla_heads), P(vla_heads), c_int, c_void_p, c_void_p, c_float, c_void_p, c_void_p,
-                                    c_int, c_void_p, P(vla_heads), P(vla_heads), c_int, c_int, c_int, c_int, c_int,
-                                    c_void_p],
-            "vla_op_kv4_store": [P(vla_heads), P(vla_heads), c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int,
-                                 c_int, c_void_p],
-            "vla_op_kv4_load": [c_void_p, c_void_p, c_void_p, P(vla_heads), P(vla_heads), c_int, c_int, c_int, c_int,
-                                c_int, c_void_p],
-            "vla_op_attention_kv4": [P(vla_heads), c_void_p, c_void_p, P(vla_heads), c_int, c_int, c_int, c_int, c_int,
-                                     c_int, c_int, c_int, c_int, c_void_p, c_size_t, c_void_p],
+            # vla_heads go in as their 32 bytes
+            "vla_op_qk_norm_rope": [c_char_p, c_char_p, c_int, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_int,
+                                    c_void_p, c_char_p, c_char_p, c_int, c_int, c_int, c_int, c_int, c_void_p],
+            "vla_op_kv4_store": [c_char_p, c_char_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
+                                 c_void_p],
+            "vla_op_kv4_load": [c_void_p, c_void_p, c_void_p, c_char_p, c_char_p, c_int, c_int, c_int, c_int, c_int,
+                                c_void_p],
+            "vla_op_attention_kv4": [c_char_p, c_void_p, c_void_p, c_char_p, c_int, c_int, c_int, c_int, c_int, c_int,
+                                     c_int, c_int, c_int, c_void_p, c_size_t, c_void_p],
             "vla_suffix_create": [P(vla_stack_cfg), c_int, c_int, c_int, P(c_void_p)],
             "vla_suffix_load_block_weights": [c_void_p, c_int, P(vla_block_weights)],
             "vla_suffix_run": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
@@ -418,58 +415,66 @@ def vla_op_gemm_tile_bf16(op, tile, A, Wp, out, bias, M, N, K, stream=None):
 
 # ----------------------------------------- 4-bit weights and KV cache (torch)
 # These calls take torch tensors on the GPU and read sizes and strides off
-# them; a tensor whose type, shape or size does not fit raises ValueError
-# before the library is called.  `stream`: a hipStream_t (torch's
-# `stream.cuda_stream`), None = the null stream.
+# them; a tensor whose type, shape, device or size does not fit raises
+# ValueError before the library is called.  `stream`: a hipStream_t (torch's
+# `stream.cuda_stream`), None = the null stream.  A decode step's kernels take
+# two to five microseconds, so the checks are written to cost little: no
+# message is built and nothing converted unless something is wrong.
 
-_DTYPES = {}
-
-
-def _dtype(t):
-    """VLA_BF16 or VLA_F32 of a tensor."""
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.bfloat16: VLA_BF16, torch.float32: VLA_F32})
-    return _DTYPES.get(t.dtype, -1)
+_HEADS = struct.Struct("Pqqq").pack  # a vla_heads
+_BF16 = _F32 = _I32 = None           # torch's types, once torch is there
+_current = None                      # the current device, where there are several
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _types():
+    import torch
+    global _BF16, _F32, _I32, _current
+    _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+    if torch.cuda.device_count() > 1:
+        _current = torch.cuda.current_device
 
 
-def _dev(t, like, what):
-    """Address of a dense tensor on `like`'s device (None: NULL)."""
+def _bad(what):
+    raise ValueError(what)
+
+
+def _device(t, what):
+    """Index of t's GPU, which has to be the current one (kernels run there)."""
+    d = t.get_device()
+    if _BF16 is None:
+        _types()
+    if d < 0:
+        _bad("%s: a tensor on the GPU is needed" % what)
+    if _current is not None and _current() != d:
+        _bad("%s: on device %d, which is not the current one" % (what, d))
+    return d
+
+
+def _dense(t, dtype, shape, dev, what):
+    """Address of a dense tensor of that type and shape (None: NULL)."""
     if t is None:
         return None
-    _need(t.is_contiguous() and t.device == like.device, "%s: a contiguous tensor on %s is needed" % (what, like.device))
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _bad("%s: a contiguous %s tensor of shape %s on the same GPU is needed" % (what, dtype, tuple(shape)))
     return t.data_ptr()
 
 
-def _int32(t, like, shape, what):
-    """Address of a dense int32 device tensor of that shape (None: NULL)."""
-    if t is None:
-        return None
-    _need(t.element_size() == 4 and not t.is_floating_point() and tuple(t.shape) == shape, "%s: int32 %s is needed" % (what, shape))
-    return _dev(t, like, what)
+def _memory(t, need, dev, what):
+    """Address of at least `need` bytes of dense memory."""
+    if t.numel() * t.element_size() < need or t.get_device() != dev or not t.is_contiguous():
+        _bad("%s: %d contiguous bytes on the same GPU are needed" % (what, need))
+    return t.data_ptr()
 
 
-def _f32(t, like, shape, what):
-    """Address of a dense fp32 device tensor of that shape (None: NULL)."""
-    if t is None:
-        return None
-    _need(_dtype(t) == VLA_F32 and tuple(t.shape) == shape, "%s: float32 %s is needed" % (what, shape))
-    return _dev(t, like, what)
-
-
-def _heads(t, shape, like, what, dtype=VLA_BF16):
-    """vla_heads over a tensor [B, tokens, heads, dh] of any outer strides."""
-    _need(tuple(t.shape) == shape and _dtype(t) == dtype and t.device == like.device and t.is_cuda,
-          "%s: %s %s on the GPU is needed" % (what, "float32" if dtype == VLA_F32 else "bfloat16", shape))
+def _heads(t, dtype, shape, dev, what):
+    """The vla_heads of a tensor [B, tokens, heads, dh] of any outer strides."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _bad("%s: a %s tensor of shape %s on the same GPU is needed" % (what, dtype, tuple(shape)))
     s = t.stride()
-    _need(s[3] == 1, "%s: the last dimension has to be dense" % what)
+    if s[3] != 1:
+        _bad("%s: the last dimension has to be dense" % what)
     # the stride of a dimension of one is never used
-    return vla_heads(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+    return _HEADS(t.data_ptr(), s[0] if shape[0] != 1 else 0, s[1] if shape[1] != 1 else 0, s[2] if shape[2] != 1 else 0)
 
 
 def vla_op_w4_packed_bytes(N, K, group):
@@ -478,78 +483,99 @@ def vla_op_w4_packed_bytes(N, K, group):
 
 def vla_op_w4_pack(codes, scales, zeros, Wp, group, stream=None):
     """codes [N, K] uint8, scales and zeros (or None) [N, ceil(K / group)]
-    bfloat16 -> Wp, a uint8 tensor of vla_op_w4_packed_bytes(N, K, group)."""
-    _need(codes.dim() == 2 and codes.element_size() == 1 and codes.is_cuda, "codes: uint8 [N, K] on the GPU is needed")
+    bfloat16 -> Wp, a tensor of vla_op_w4_packed_bytes(N, K, group) bytes."""
+    dev = _device(codes, "codes")
+    if codes.dim() != 2 or codes.element_size() != 1 or not codes.is_contiguous() or group <= 0:
+        _bad("codes: contiguous uint8 [N, K] and a group size are needed")
     N, K = codes.shape
-    need = vla_op_w4_packed_bytes(N, K, group)
-    for t, what in ((scales, "scales"), (zeros, "zeros")):
-        _need(t is None or (_dtype(t) == VLA_BF16 and tuple(t.shape) == (N, -(-K // max(group, 1)))),
-              "%s: bfloat16 [N, ceil(K / group)] is needed" % what)
-    _need(Wp.numel() * Wp.element_size() >= need, "Wp: %d bytes are needed" % need)
-    _check(lib().vla_op_w4_pack(_dev(codes, codes, "codes"), _dev(scales, codes, "scales"), _dev(zeros, codes, "zeros"),
-                                _dev(Wp, codes, "Wp"), N, K, group, stream))
+    per = (N, -(-K // group))
+    _check(lib().vla_op_w4_pack(codes.data_ptr(), _dense(scales, _BF16, per, dev, "scales"),
+                                _dense(zeros, _BF16, per, dev, "zeros"),
+                                _memory(Wp, vla_op_w4_packed_bytes(N, K, group), dev, "Wp"), N, K, group, stream))
 
 
 def vla_op_gemv_w4(x, Wp, residual, out, N, group, swiglu=False, stream=None):
     """x [M, K] bfloat16 and residual (None or float32), out [M, N or N / 2]
     (float32 or bfloat16), rows of any stride; residual's rows and out's are
     equally far apart."""
-    _need(x.dim() == 2 and _dtype(x) == VLA_BF16 and x.stride(1) == 1 and x.is_cuda, "x: bfloat16 [M, K] on the GPU is needed")
+    dev = _device(x, "x")
+    L = lib()
+    if x.dtype is not _BF16 or x.dim() != 2 or x.stride(1) != 1:
+        _bad("x: bfloat16 [M, K] with dense rows is needed")
     M, K = x.shape
     wide = (M, N // 2 if swiglu else N)
-    _need(tuple(out.shape) == wide and out.stride(1) == 1 and _dtype(out) >= 0 and out.device == x.device,
-          "out: float32 or bfloat16 %s is needed" % (wide,))
-    ldo = out.stride(0) if M > 1 else 0
+    f32 = out.dtype is _F32
+    if not (f32 or out.dtype is _BF16) or out.shape != wide or out.stride(1) != 1 or out.get_device() != dev:
+        _bad("out: float32 or bfloat16 %s with dense rows on the same GPU is needed" % (wide,))
+    ldx, ldo = (x.stride(0), out.stride(0)) if M > 1 else (0, 0)
     res = None
     if residual is not None:
-        _need(tuple(residual.shape) == wide and _dtype(residual) == VLA_F32 and residual.stride(1) == 1
-              and residual.device == x.device and (M == 1 or residual.stride(0) == ldo),
-              "residual: float32 %s with out's row stride is needed" % (wide,))
+        if (residual.dtype is not _F32 or residual.shape != wide or residual.stride(1) != 1
+                or residual.get_device() != dev or (M > 1 and residual.stride(0) != ldo)):
+            _bad("residual: float32 %s with out's row stride on the same GPU is needed" % (wide,))
         res = residual.data_ptr()
-    _need(Wp.numel() * Wp.element_size() >= vla_op_w4_packed_bytes(N, K, group), "Wp: not the packed weights of these sizes")
-    _check(lib().vla_op_gemv_w4(x.data_ptr(), x.stride(0) if M > 1 else 0, _dev(Wp, x, "Wp"), res, out.data_ptr(), ldo,
-                                _dtype(out), int(swiglu), M, N, K, group, stream))
+    code = L.vla_op_gemv_w4(x.data_ptr(), ldx, _memory(Wp, L.vla_op_w4_packed_bytes(N, K, group), dev, "Wp"), res,
+                            out.data_ptr(), ldo, f32, bool(swiglu), M, N, K, group, stream)
+    if code:
+        _check(code)
 
 
 def vla_op_qk_norm_rope(q, k, gq, gk, eps, cos, sin, pos, q_out, k_out, stream=None):
     """q, q_out [B, L, H, dh], k, k_out [B, L, Hkv, dh] (inputs bfloat16 or
     float32, outputs bfloat16), gq, gk [dh] and cos, sin [n_pos, dh / 2]
     float32 or None, pos [B, L] int32 or None."""
-    _need(q.dim() == 4 and k.dim() == 4 and q.is_cuda, "q, k: [B, L, heads, dh] on the GPU are needed")
-    B, L, H, dh = q.shape
-    kshape = (B, L, k.shape[2], dh)
+    dev = _device(q, "q")
+    dt = q.dtype
+    qs, ks = q.shape, k.shape
+    if not (dt is _F32 or dt is _BF16) or len(qs) != 4 or len(ks) != 4:
+        _bad("q, k: float32 or bfloat16 [B, L, heads, dh] are needed")
+    B, L, H, dh = qs
+    ks = (B, L, ks[2], dh)
     n_pos = 0 if cos is None else cos.shape[0]
-    dt = _dtype(q)
-    _check(lib().vla_op_qk_norm_rope(_heads(q, (B, L, H, dh), q, "q", dt), _heads(k, kshape, q, "k", dt), dt,
-                                     _f32(gq, q, (dh,), "gq"), _f32(gk, q, (dh,), "gk"), eps,
-                                     _f32(cos, q, (n_pos, dh // 2), "cos"), _f32(sin, q, (n_pos, dh // 2), "sin"), n_pos,
-                                     _int32(pos, q, (B, L), "pos"), _heads(q_out, (B, L, H, dh), q, "q_out"),
-                                     _heads(k_out, kshape, q, "k_out"), B, L, H, k.shape[2], dh, stream))
+    code = lib().vla_op_qk_norm_rope(
+        _heads(q, dt, qs, dev, "q"), _heads(k, dt, ks, dev, "k"), dt is _F32, _dense(gq, _F32, (dh,), dev, "gq"),
+        _dense(gk, _F32, (dh,), dev, "gk"), eps, _dense(cos, _F32, (n_pos, dh // 2), dev, "cos"),
+        _dense(sin, _F32, (n_pos, dh // 2), dev, "sin"), n_pos, _dense(pos, _I32, (B, L), dev, "pos"),
+        _heads(q_out, _BF16, qs, dev, "q_out"), _heads(k_out, _BF16, ks, dev, "k_out"), B, L, H, ks[2], dh, stream)
+    if code:
+        _check(code)
 
 
 def vla_op_kv4_bytes(B, Hkv, L_cap, dh):
     return lib().vla_op_kv4_bytes(B, Hkv, L_cap, dh)
 
 
-def _kv4_rows(k, v, start, count, cache, L_cap):
-    _need(k.dim() == 4 and k.is_cuda, "k: [B, L, Hkv, dh] on the GPU is needed")
-    B, L, Hkv, dh = shape = tuple(k.shape)
-    _need(cache.numel() * cache.element_size() >= vla_op_kv4_bytes(B, Hkv, L_cap, dh), "cache: not of these sizes")
-    return (_heads(k, shape, k, "k"), _heads(v, shape, k, "v"), _int32(start, k, (B,), "start"),
-            _int32(count, k, (B,), "count"), _dev(cache, k, "cache"), (B, L, Hkv, L_cap, dh))
-
-
 def vla_op_kv4_store(k, v, start, count, cache, L_cap, stream=None):
     """k, v [B, L, Hkv, dh] bfloat16, start, count [B] int32 or None, cache a
-    uint8 tensor of vla_op_kv4_bytes(B, Hkv, L_cap, dh)."""
-    k, v, start, count, cache, sizes = _kv4_rows(k, v, start, count, cache, L_cap)
-    _check(lib().vla_op_kv4_store(k, v, start, count, cache, *sizes, stream))
+    tensor of vla_op_kv4_bytes(B, Hkv, L_cap, dh) bytes."""
+    dev = _device(k, "k")
+    L = lib()
+    shape = k.shape
+    if len(shape) != 4:
+        _bad("k: [B, L, Hkv, dh] is needed")
+    B, n, Hkv, dh = shape
+    code = L.vla_op_kv4_store(
+        _heads(k, _BF16, shape, dev, "k"), _heads(v, _BF16, shape, dev, "v"), _dense(start, _I32, (B,), dev, "start"),
+        _dense(count, _I32, (B,), dev, "count"), _memory(cache, L.vla_op_kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), B,
+        n, Hkv, L_cap, dh, stream)
+    if code:
+        _check(code)
 
 
 def vla_op_kv4_load(cache, L_cap, start, count, k, v, stream=None):
     """The inverse of vla_op_kv4_store, into k and v."""
-    k, v, start, count, cache, sizes = _kv4_rows(k, v, start, count, cache, L_cap)
-    _check(lib().vla_op_kv4_load(cache, start, count, k, v, *sizes, stream))
+    dev = _device(k, "k")
+    L = lib()
+    shape = k.shape
+    if len(shape) != 4:
+        _bad("k: [B, L, Hkv, dh] is needed")
+    B, n, Hkv, dh = shape
+    code = L.vla_op_kv4_load(
+        _memory(cache, L.vla_op_kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), _dense(start, _I32, (B,), dev, "start"),
+        _dense(count, _I32, (B,), dev, "count"), _heads(k, _BF16, shape, dev, "k"), _heads(v, _BF16, shape, dev, "v"), B,
+        n, Hkv, L_cap, dh, stream)
+    if code:
+        _check(code)
 
 
 def vla_op_attention_kv4_scratch(B, Lq, H, Hkv, dh, max_len, window=0, sinks=0):
@@ -557,15 +583,21 @@ def vla_op_attention_kv4_scratch(B, Lq, H, Hkv, dh, max_len, window=0, sinks=0):
 
 
 def vla_op_attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window=0, sinks=0, scratch=None, stream=None):
-    """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a uint8 tensor of
+    """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a tensor of
     vla_op_attention_kv4_scratch(...) bytes (None where that is 0)."""
-    _need(q.dim() == 4 and q.is_cuda and lens is not None, "q [B, Lq, H, dh] and lens [B] on the GPU are needed")
-    B, Lq, H, dh = shape = tuple(q.shape)
-    _need(cache.numel() * cache.element_size() >= vla_op_kv4_bytes(B, Hkv, L_cap, dh), "cache: not of these sizes")
+    dev = _device(q, "q")
+    L = lib()
+    shape = q.shape
+    if len(shape) != 4 or lens is None:
+        _bad("q [B, Lq, H, dh] and lens [B] are needed")
+    B, Lq, H, dh = shape
     nbytes = 0 if scratch is None else scratch.numel() * scratch.element_size()
-    _check(lib().vla_op_attention_kv4(_heads(q, shape, q, "q"), _dev(cache, q, "cache"), _int32(lens, q, (B,), "lens"),
-                                      _heads(o, shape, q, "o"), B, Lq, H, Hkv, L_cap, dh, max_len, window, sinks,
-                                      _dev(scratch, q, "scratch") if nbytes else None, nbytes, stream))
+    code = L.vla_op_attention_kv4(
+        _heads(q, _BF16, shape, dev, "q"), _memory(cache, L.vla_op_kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"),
+        _dense(lens, _I32, (B,), dev, "lens"), _heads(o, _BF16, shape, dev, "o"), B, Lq, H, Hkv, L_cap, dh, max_len,
+        window, sinks, _memory(scratch, nbytes, dev, "scratch") if nbytes else None, nbytes, stream)
+    if code:
+        _check(code)
 
 
 def vla_status_string(code: int) -> str:

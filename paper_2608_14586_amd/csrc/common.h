@@ -38,4 +38,29 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
+// A value of another lane by DPP: CTRL 0xB1 and 0x4E exchange lanes 1 and 2
+// apart, 0x141 and 0x140 mirror a row's halves and the row (16 lanes), so that
+// after the first n of the four every 2^n lanes have met.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+// over the N (4, 8 or 16) lanes that lie side by side
+template <int N = 16>
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, dpp<0xB1>(x));
+  x = fmaxf(x, dpp<0x4E>(x));
+  if constexpr (N > 4) x = fmaxf(x, dpp<0x141>(x));
+  if constexpr (N > 8) x = fmaxf(x, dpp<0x140>(x));
+  return x;
+}
+template <int N = 16>
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0xB1>(x);
+  x += dpp<0x4E>(x);
+  if constexpr (N > 4) x += dpp<0x141>(x);
+  if constexpr (N > 8) x += dpp<0x140>(x);
+  return x;
+}
+
 static constexpr inline int cdiv(int a, int b) { return (a + b - 1) / b; }

@@ -149,6 +149,17 @@ hipError_t decode_down(const bf16_t* a, int fpad, const WOperand& W, float* h, i
                        int parts = 1);
 
 // ------------------------------------------------- 4-bit weights and KV cache
+// n / d for 0 <= n < 2^31 as (n m) >> s: m = ceil(2^s / d), s = 31 + ceil(log2 d)
+struct FastDiv {
+  uint32_t m, s;
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t s = 31;
+  while ((1ull << (s - 31)) < d) ++s;
+  return {(uint32_t)(((1ull << s) + d - 1) / d), s};
+}
+__device__ __forceinline__ int div_by(int n, const FastDiv& d) { return (int)((uint64_t)(uint32_t)n * d.m >> d.s); }
+
 // Head rows of a call: element (b, token, head, d) at p + b * seq + token *
 // this->token + head * this->head + d, strides in elements.
 struct Heads {
@@ -176,8 +187,9 @@ struct QkNormArgs {
   const int32_t* pos;
   float eps;
   int n_pos, B, L, H, Hkv;
+  FastDiv by_L;  // filled in by the launch
 };
-hipError_t qk_norm_rope(const QkNormArgs& a, bool f32, int dh, hipStream_t s);
+hipError_t qk_norm_rope(QkNormArgs a, bool f32, int dh, hipStream_t s);
 
 // Rows of k, v [B][L][Hkv][dh] into (store) or out of (load) the 4-bit cache
 // (kv4.hip), positions start[b] .. start[b] + count[b] - 1 (NULL: 0, L).
@@ -186,15 +198,13 @@ struct Kv4Rows {
   void* cache;
   const int32_t *start, *count;
   int B, L, Hkv, L_cap;
+  int blocks;  // a sequence's rows can touch; with the divisors filled in by the launch
+  FastDiv by_blocks, by_Hkv;
 };
 size_t kv4_bytes(int B, int Hkv, int L_cap, int dh);
-hipError_t kv4_store(const Kv4Rows& a, int dh, hipStream_t s);
-hipError_t kv4_load(const Kv4Rows& a, int dh, hipStream_t s);
+hipError_t kv4_store(Kv4Rows a, int dh, hipStream_t s);
+hipError_t kv4_load(Kv4Rows a, int dh, hipStream_t s);
 
-// n / d for 0 <= n < 2^31 as (n m) >> s: m = ceil(2^s / d), s = 31 + ceil(log2 d)
-struct FastDiv {
-  uint32_t m, s;
-};
 // Attention of the last Lq of lens[b] cached tokens over the 4-bit cache;
 // what comes after `sinks` is filled in by the launch.
 struct Kv4Attn {

@@ -28,6 +28,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+constexpr uint32_t ONES = 0x3f803f80u;  // bf16 1.0 twice
 constexpr int BLK = 32;  // tokens per block
 constexpr float RAISE = 8.f;  // log2 by which a weight may exceed 1
 constexpr int KROT = 3, VROT = 6;
@@ -65,19 +66,35 @@ struct Group4 {
   uint32_t codes;   // of this lane's 8 dims
   uint32_t params;  // of the group
 };
+// The codes of 8 values whose group spans [lo, lo + d], with step s and its
+// approximate inverse.  The quotient is corrected once by its remainder: x -
+// lo and s have at most 17 and 8 significant bits, so a quotient on a border
+// between two codes is exactly representable and comes out exact; s lies within
+// 2^-9 of d / 15, so none rounds to more than 15.  Halves of a word are summed
+// up in fp32, 16 bits each.
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float lo, float s, float inv) {
+  float half[2] = {0.f, 0.f};
+#pragma unroll
+  for (int e = 7; e >= 0; --e) {
+    const float t = x[e] - lo;
+    float q = t * inv;
+    q = rintf(fmaf(fmaf(-q, s, t), inv, q));
+    half[e & 1] = fmaf(half[e & 1], 16.f, q);
+  }
+  return (uint32_t)half[0] | (uint32_t)half[1] << 16;
+}
 // Quantises the 8 dims of this lane; the 4 lanes of a group hold its 32 dims.
-// Half of every number is used, so that max - min cannot overflow.  The
-// quotient is corrected once by its remainder: x - m and s have at most 17
-// and 8 significant bits, so a quotient that lies on a border between codes
-// is exactly representable, and comes out exact.
 __device__ __forceinline__ Group4 quantise(const u32x4& w) {
-  float x[8];
-  uint32_t mag = 0;
+  float x[8], any = 0.f;  // any: a sum that is finite only if all values are
+  const bf16x8 v = __builtin_bit_cast(bf16x8, w), one = __builtin_bit_cast(bf16x8, u32x4{ONES, ONES, ONES, ONES});
+  any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(v, v, 0, 1), __builtin_shufflevector(one, one, 0, 1), any, false);
+  any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(v, v, 2, 3), __builtin_shufflevector(one, one, 0, 1), any, false);
+  any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(v, v, 4, 5), __builtin_shufflevector(one, one, 0, 1), any, false);
+  any = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(v, v, 6, 7), __builtin_shufflevector(one, one, 0, 1), any, false);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[2 * e] = lo16(w[e]);
     x[2 * e + 1] = hi16(w[e]);
-    mag = max(mag, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
   }
   float lo = x[0], hi = x[0];
 #pragma unroll
@@ -85,40 +102,75 @@ __device__ __forceinline__ Group4 quantise(const u32x4& w) {
     lo = fminf(lo, x[e]);
     hi = fmaxf(hi, x[e]);
   }
-#pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    lo = fminf(lo, __shfl_xor(lo, o));
-    hi = fmaxf(hi, __shfl_xor(hi, o));
-    mag = max(mag, (uint32_t)__shfl_xor((int)mag, o));
-  }
-  if (mag >= 0x7f80u) return Group4{0u, 0x7fc07fc0u};  // a value that is not finite: the group reads as NaN
-  const float half = 0.5f * hi - 0.5f * lo;
+  lo = -row_max<4>(-lo);
+  hi = row_max<4>(hi);
+  any = row_sum<4>(any);
+  const float d = hi - lo;
   const uint32_t m = __float_as_uint(lo) & 0xffff0000u;
-  if (!(half >= 0x1p-100f)) return Group4{0u, m};
-  const uint16_t sb = f2bf(half / 7.5f);
-  const float hs = 0.5f * bf2f(sb), inv = 1.f / hs;
-  uint32_t c = 0;
+  // where a value or a sum of values is not finite: once more with care
+  if (!(fabsf(any) <= 3.4e38f && d <= 3.4e38f)) {
+    uint32_t mag = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float t = fmaf(0.5f, x[e], -0.5f * lo);
-    float q = t * inv;
-    q = fmaf(fmaf(-q, hs, t), inv, q);
-    c |= (uint32_t)fminf(rintf(q), 15.f) << 4 * (e / 2 + (e & 1) * 4);
+    for (int e = 0; e < 4; ++e) mag = max(mag, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+    // of the group; the condition above is the same in its 4 lanes
+    if (row_max<4>((float)mag) >= (float)0x7f80) return Group4{0u, 0x7fc07fc0u};  // the group reads as NaN
+    if (!(d <= 3.4e38f)) {  // a range past fp32: everything by halves
+      const float half = 0.5f * hi - 0.5f * lo;
+      const uint16_t sb = f2bf(half / 7.5f);
+      const float hs = 0.5f * bf2f(sb);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= 0.5f;
+      return Group4{codes_of(x, 0.5f * lo, hs, 1.f / hs), m | sb};
+    }
   }
-  return Group4{c, m | sb};
+  if (!(d >= 0x1p-99f)) return Group4{0u, m};
+  // d / 15, corrected once: correctly rounded
+  float s = d * (1.f / 15);
+  s = fmaf(fmaf(-s, 15.f, d), 1.f / 15, s);
+  const uint16_t sb = f2bf(s);
+  s = bf2f(sb);
+  return Group4{codes_of(x, lo, s, __builtin_amdgcn_rcpf(s)), m | sb};
 }
+
+// Transposes 8 x 8 codes of 4 bits: nibble c of word r becomes nibble r of word c.
+__device__ __forceinline__ void transpose8(uint32_t (&w)[8]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint32_t a = w[r], b = w[r + 4];
+    w[r] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    w[r + 4] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  }
+#pragma unroll
+  for (int r = 0; r < 8; r += r % 2 ? 3 : 1) {
+    const uint32_t a = w[r], b = w[r + 2];
+    w[r] = __builtin_amdgcn_perm(b, a, 0x06020400u);
+    w[r + 2] = __builtin_amdgcn_perm(b, a, 0x07030501u);
+  }
+#pragma unroll
+  for (int r = 0; r < 8; r += 2) {
+    const uint32_t a = w[r], b = w[r + 1];
+    w[r] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
+    w[r + 1] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
+  }
+}
+// dim 8 j + e of a token is code nibble_of(e) of its word j
+__host__ __device__ constexpr int nibble_of(int e) { return e / 2 + (e & 1) * 4; }
+__host__ __device__ constexpr int dim_of(int nibble) { return nibble % 4 * 2 + nibble / 4; }
+// token i of a quarter's eight is token_of(quarter, i) of the block
+__device__ __forceinline__ int token_of(int quarter, int i) { return 4 * quarter + i % 4 + i / 4 * 16; }
 
 // this workgroup's block of the cache and the tokens of the call in it:
 // tokens [t0, t1) of the block are tokens from + (t - t0) of the sequence's rows
 struct Span {
   int b, h, blk, t0, t1, from;
 };
-__device__ __forceinline__ Span span_of(const Kv4Rows& a) {
+__device__ __forceinline__ Span span_of(const Kv4Rows& a, int wg) {
   Span s;
-  const int nb = a.L / BLK + 2;
-  const int i = blockIdx.x % nb, bh = blockIdx.x / nb;
-  s.h = bh % a.Hkv;
-  s.b = bh / a.Hkv;
+  // the heads of a block side by side: so are their rows of a token, where heads are inner
+  const int bi = div_by(wg, a.by_Hkv);
+  s.h = wg - bi * a.Hkv;
+  s.b = div_by(bi, a.by_blocks);
+  const int i = bi - s.b * a.blocks;
   const int64_t start = a.start ? a.start[s.b] : 0;
   const int count = a.count ? min(max(a.count[s.b], 0), a.L) : a.L;
   // rows [first, last) of the cache, cut to the rows that it has
@@ -132,82 +184,113 @@ __device__ __forceinline__ Span span_of(const Kv4Rows& a) {
   return s;
 }
 
+// One workgroup for the keys of a block of 32 tokens of a head (even ones) or
+// for its values; DH / 8 lanes a row.  About 110 instructions a lane and 8
+// values take as long as the memory does, so there are workgroups enough for
+// two rounds, whose loads and arithmetic overlap.  The value codes cross LDS
+// to the threads that hold 8 dims of 8 tokens and transpose them.
 template <int DH>
 __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows a) {
-  constexpr int LPR = DH / 8, RPP = 256 / LPR, NG = DH / 32, ND = DH / 16;  // lanes a row, rows a pass
+  constexpr int LPR = DH / 8, RPP = 256 / LPR, P = BLK / RPP, NG = DH / 32, ND = DH / 16;  // lanes a row, rows a pass
   __shared__ uint32_t vs[BLK][LPR];
-  const Span s = span_of(a);
+  const Span s = span_of(a, blockIdx.x >> 1);
+  const bool values = blockIdx.x & 1;
   if (s.t0 >= s.t1) return;
   uint8_t* base = (uint8_t*)a.cache + (((size_t)s.b * a.Hkv + s.h) * (a.L_cap / BLK) + s.blk) * (40 * DH);
   const int tid = threadIdx.x, j = tid % LPR, g = j / 4, kq = j % 4;
+  const Heads& in = values ? a.v : a.k;
+  u32x4 x[P];
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const Heads& in = p ? a.v : a.k;
-#pragma unroll
-    for (int r = 0; r < BLK / RPP; ++r) {
-      const int t = r * RPP + tid / LPR;
-      if (t < s.t0 || t >= s.t1) continue;
-      const bf16_t* row = (const bf16_t*)in.p + s.b * in.seq + (int64_t)(s.from + t - s.t0) * in.token + s.h * in.head;
-      const Group4 q = quantise(*(const u32x4*)(row + j * 8));
-      if (p)
-        vs[t][j] = q.codes;
-      else
-        *(uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4) = rotl(q.codes, KROT);
-      if (kq == 0) *(uint32_t*)(base + (p ? 36 : 32) * DH + (t * NG + g) * 4) = q.params;
-    }
+  for (int r = 0; r < P; ++r) {
+    const int t = r * RPP + tid / LPR;
+    if (t >= s.t0 && t < s.t1)
+      x[r] = *(const u32x4*)((const bf16_t*)in.p + s.b * in.seq + (int64_t)(s.from + t - s.t0) * in.token +
+                             s.h * in.head + j * 8);
   }
-  __syncthreads();
   uint32_t* vc = (uint32_t*)(base + 16 * DH);
-  for (int i = tid; i < 4 * DH; i += 256) {
-    const int d = i % ND * 16 + i / ND % 16, q4 = i / DH * 4;
-    const int sh = 4 * (d % 8 / 2 + (d & 1) * 4);
-    uint32_t w = 0, have = 0;
+  auto word_at = [&](int c) {  // of value code words of quarter tid / LPR
+    const int d = j * 8 + dim_of(c);
+    return (tid / LPR * 16 + d % 16) * ND + d / 16;
+  };
+  uint32_t old[8];  // of a block that the call does not fill
+  if (values && s.t1 - s.t0 < BLK && tid < 4 * LPR)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int t = q4 + e % 4 + e / 4 * 16;
-      if (t >= s.t0 && t < s.t1) {
-        w |= (vs[t][d / 8] >> sh & 15u) << 4 * e;
-        have |= 15u << 4 * e;
-      }
-    }
-    if (have == 0) continue;
-    if (have != 0xffffffffu) w |= rotl(vc[i], 32 - VROT) & ~have;  // tokens of other calls keep theirs
-    vc[i] = rotl(w, VROT);
+    for (int c = 0; c < 8; ++c) old[c] = vc[word_at(c)];
+#pragma unroll
+  for (int r = 0; r < P; ++r) {
+    const int t = r * RPP + tid / LPR;
+    if (t < s.t0 || t >= s.t1) continue;
+    const Group4 q = quantise(x[r]);
+    if (values)
+      vs[t][j] = q.codes;
+    else
+      *(uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4) = rotl(q.codes, KROT);
+    if (kq == 0) *(uint32_t*)(base + (values ? 36 : 32) * DH + (t * NG + g) * 4) = q.params;
+  }
+  if (!values) return;
+  __syncthreads();
+  if (tid >= 4 * LPR) return;
+  const int q4 = tid / LPR;
+  uint32_t w[8], have = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int t = token_of(q4, i);
+    const bool there = t >= s.t0 && t < s.t1;
+    w[i] = there ? vs[t][j] : 0u;
+    have |= there ? 15u << 4 * i : 0u;
+  }
+  if (have == 0) return;
+  transpose8(w);
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    if (have != 0xffffffffu) w[c] |= rotl(old[c], 32 - VROT) & ~have;  // tokens of other calls keep theirs
+    vc[word_at(c)] = rotl(w[c], VROT);
   }
 }
 
+// The inverse: 4 DH / 8 threads transpose the block's value codes into LDS,
+// word j of every token as the keys have it.
 template <int DH>
 __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
-  constexpr int LPR = DH / 8, RPP = 256 / LPR, NG = DH / 32, ND = DH / 16;
-  __shared__ uint32_t vs[4 * DH];
-  const Span s = span_of(a);
+  constexpr int LPR = DH / 8, RPP = 256 / LPR, P = BLK / RPP, NG = DH / 32, ND = DH / 16;
+  __shared__ uint32_t vs[BLK][LPR];
+  const Span s = span_of(a, blockIdx.x);
   if (s.t0 >= s.t1) return;
   const uint8_t* base = (const uint8_t*)a.cache + (((size_t)s.b * a.Hkv + s.h) * (a.L_cap / BLK) + s.blk) * (40 * DH);
   const int tid = threadIdx.x, j = tid % LPR, g = j / 4, kq = j % 4;
-  for (int i = tid; i < 4 * DH; i += 256) vs[i] = rotl(((const uint32_t*)(base + 16 * DH))[i], 32 - VROT);
+  uint32_t kw[P], prm[2][P];
+#pragma unroll
+  for (int r = 0; r < P; ++r) {
+    const int t = r * RPP + tid / LPR;
+    kw[r] = *(const uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) prm[p][r] = *(const uint32_t*)(base + (p ? 36 : 32) * DH + (t * NG + g) * 4);
+  }
+  if (tid < 4 * LPR) {
+    const int q4 = tid / LPR;
+    uint32_t w[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const int d = j * 8 + dim_of(c);
+      w[c] = rotl(((const uint32_t*)(base + 16 * DH))[(q4 * 16 + d % 16) * ND + d / 16], 32 - VROT);
+    }
+    transpose8(w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vs[token_of(q4, i)][j] = w[i];
+  }
   __syncthreads();
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     const Heads& out = p ? a.v : a.k;
 #pragma unroll
-    for (int r = 0; r < BLK / RPP; ++r) {
+    for (int r = 0; r < P; ++r) {
       const int t = r * RPP + tid / LPR;
       if (t < s.t0 || t >= s.t1) continue;
-      const uint32_t prm = *(const uint32_t*)(base + (p ? 36 : 32) * DH + (t * NG + g) * 4);
-      const float sc = lo16(prm), mn = hi16(prm);
-      const uint32_t kw = p ? 0u : rotl(*(const uint32_t*)(base + t * (DH / 2) + kq * (DH / 8) + g * 4), 32 - KROT);
+      const uint32_t w = p ? vs[t][j] : rotl(kw[r], 32 - KROT);
+      const float sc = lo16(prm[p][r]), mn = hi16(prm[p][r]);
       float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint32_t c;
-        if (p) {
-          const int d = j * 8 + e, w = (t % 16 / 4) * DH + (d % 16) * ND + d / 16;
-          c = vs[w] >> 4 * (t % 4 + t / 16 * 4) & 15u;
-        } else {
-          c = kw >> 4 * (e / 2 + (e & 1) * 4) & 15u;
-        }
-        x[e] = fmaf(sc, (float)c, mn);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = fmaf(sc, (float)(w >> 4 * nibble_of(e) & 15u), mn);
       bf16_t* row = (bf16_t*)out.p + s.b * out.seq + (int64_t)(s.from + t - s.t0) * out.token + s.h * out.head;
       *(u32x4*)(row + j * 8) =
           u32x4{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(x[4], x[5]), pack_bf2(x[6], x[7])};
@@ -242,35 +325,17 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // 32 keys, workgroups contiguous runs of them, joined in LDS and by
 // kv4_combine_kernel.
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
-}
 // a value of one lane, for all
 __device__ __forceinline__ float lane_of(float x, int lane) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane));
 }
-// over the 16 lanes of a row
-__device__ __forceinline__ float row_max(float x) {
-  x = fmaxf(x, dpp<0xB1>(x));
-  x = fmaxf(x, dpp<0x4E>(x));
-  x = fmaxf(x, dpp<0x141>(x));
-  return fmaxf(x, dpp<0x140>(x));
-}
-__device__ __forceinline__ float row_sum(float x) {
-  x += dpp<0xB1>(x);
-  x += dpp<0x4E>(x);
-  x += dpp<0x141>(x);
-  return x + dpp<0x140>(x);
-}
-
 // over the wave
 __device__ __forceinline__ float wave_max(float x) {
-  x = row_max(x);
+  x = row_max<>(x);
   return fmaxf(fmaxf(lane_of(x, 0), lane_of(x, 16)), fmaxf(lane_of(x, 32), lane_of(x, 48)));
 }
 __device__ __forceinline__ float wave_sum(float x) {
-  x = row_sum(x);
+  x = row_sum<>(x);
   return (lane_of(x, 0) + lane_of(x, 16)) + (lane_of(x, 32) + lane_of(x, 48));
 }
 
@@ -299,7 +364,6 @@ __device__ __forceinline__ Words<N> load_words(__amdgpu_buffer_rsrc_t r, uint32_
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ int div_by(int n, const FastDiv& d) { return (int)((uint64_t)(uint32_t)n * d.m >> d.s); }
 // 1 / x of a power of two from 2^-126 to 2^126
 __device__ __forceinline__ float inverse2(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 
@@ -483,7 +547,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     bool raise = false;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      up[r] = row_max(fmaxf(p[0][r], p[1][r]));
+      up[r] = row_max<>(fmaxf(p[0][r], p[1][r]));
       raise |= up[r] > m[r] + RAISE;
     }
     float most = fmaxf(vs[0][0], vs[1][0]);
@@ -494,7 +558,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         // 1 / unit: the power of two above the largest step so far
-        const uint32_t e = __float_as_uint(row_max(fmaxf(steps[0][g], steps[1][g]))) & 0x7f800000u;
+        const uint32_t e = __float_as_uint(row_max<>(fmaxf(steps[0][g], steps[1][g]))) & 0x7f800000u;
         const float u = fminf(unit[g], e && e < 0x7f800000u ? __uint_as_float(0x7e800000u - e) : 0x1p126f);
         f[g] = u * inverse2(unit[g]);
         unit[g] = u;
@@ -561,7 +625,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
   float* ow = (float*)lds[wave];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const float ls = row_sum(l[r]);
+    const float ls = row_sum<>(l[r]);
     const int row = kq * R + r;
     if (c16 == 0) {
       sm[wave][row] = m[r];
@@ -569,7 +633,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float bs = row_sum(bias[r][g]), w = inverse2(unit[g]);
+      const float bs = row_sum<>(bias[r][g]), w = inverse2(unit[g]);
 #pragma unroll
       for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = fmaf(o[d][r], w, bs);
     }
@@ -656,12 +720,6 @@ __global__ __launch_bounds__(64) void kv4_combine_kernel(Kv4Attn a, int total) {
     *o = f2bf(v[0] * f);
 }
 
-FastDiv fast_div(uint32_t d) {
-  uint32_t s = 31;
-  while ((1ull << (s - 31)) < d) ++s;
-  return {(uint32_t)(((1ull << s) + d - 1) / d), s};
-}
-
 struct Plan {
   int R, W, tiles, chunk, nsplit;
 };
@@ -722,8 +780,18 @@ hipError_t by_rows(const Kv4Attn& a, const Plan& p, hipStream_t s) {
 
 size_t kv4_bytes(int B, int Hkv, int L_cap, int dh) { return (size_t)B * Hkv * (L_cap / BLK) * (40 * dh); }
 
-hipError_t kv4_store(const Kv4Rows& a, int dh, hipStream_t s) {
-  const dim3 grid((unsigned)(a.B * a.Hkv * (a.L / BLK + 2))), block(256);
+namespace {
+// blocks that L tokens from any position on can touch
+unsigned rows_grid(Kv4Rows& a) {
+  a.blocks = (a.L + 2 * (BLK - 1)) / BLK;
+  a.by_blocks = fast_div(a.blocks);
+  a.by_Hkv = fast_div(a.Hkv);
+  return (unsigned)(a.B * a.Hkv * a.blocks);
+}
+}  // namespace
+
+hipError_t kv4_store(Kv4Rows a, int dh, hipStream_t s) {
+  const dim3 grid(2 * rows_grid(a)), block(256);
   if (dh == 128)
     hipLaunchKernelGGL((kv4_store_kernel<128>), grid, block, 0, s, a);
   else
@@ -731,8 +799,8 @@ hipError_t kv4_store(const Kv4Rows& a, int dh, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t kv4_load(const Kv4Rows& a, int dh, hipStream_t s) {
-  const dim3 grid((unsigned)(a.B * a.Hkv * (a.L / BLK + 2))), block(256);
+hipError_t kv4_load(Kv4Rows a, int dh, hipStream_t s) {
+  const dim3 grid(rows_grid(a)), block(256);
   if (dh == 128)
     hipLaunchKernelGGL((kv4_load_kernel<128>), grid, block, 0, s, a);
   else

@@ -49,9 +49,9 @@ vla_status kv4_rows(const vla_heads* k, const vla_heads* v, const int32_t* start
   const vla_status st = kv4_check(B, Hkv, L_cap, dh);
   if (st != VLA_OK) return st;
   if (!heads_ok(*k) || !heads_ok(*v) || !aligned(cache, 16) || !aligned(start, 4) || !aligned(count, 4) ||
-      (int64_t)B * Hkv * (L / 32 + 2) > MAX_GRID)
+      (int64_t)B * Hkv * ((L + 62ll) / 32) > MAX_GRID)
     return VLA_ERR_UNSUPPORTED;
-  *a = vla::Kv4Rows{heads(*k), heads(*v), cache, start, count, B, L, Hkv, L_cap};
+  *a = vla::Kv4Rows{heads(*k), heads(*v), cache, start, count, B, L, Hkv, L_cap, 0, {}, {}};
   return VLA_OK;
 }
 
@@ -196,7 +196,7 @@ vla_status vla_op_qk_norm_rope(const vla_heads* q, const vla_heads* k, vla_dtype
     return VLA_ERR_UNSUPPORTED;
   if (B == 0 || L == 0) return VLA_OK;
   const vla::QkNormArgs a{heads(*q), heads(*k), heads(*q_out), heads(*k_out), gq, gk, cos, sin, pos, eps, n_pos,
-                          B, L, H, Hkv};
+                          B, L, H, Hkv, {}};
   return status_of(vla::qk_norm_rope(a, in_dtype == VLA_F32, dh, (hipStream_t)stream));
 }
 
@@ -238,7 +238,8 @@ vla_status vla_op_attention_kv4(const vla_heads* q, const void* cache, const int
     return VLA_ERR_UNSUPPORTED;
   if (B == 0 || Lq == 0) return VLA_OK;
   if (!scratch && scratch_bytes) return VLA_ERR_INVALID_ARG;
-  const vla::Kv4Attn a{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks};
+  const vla::Kv4Attn a{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks,
+                       0, 0, 0, {}, {}, {}, {}, 0.f};
   const hipError_t e = vla::kv4_attention(a, dh, scratch_bytes, (hipStream_t)stream);
   return e == hipErrorOutOfMemory ? VLA_ERR_SHAPE : status_of(e);
 }

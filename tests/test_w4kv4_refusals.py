@@ -1,6 +1,6 @@
 """What the 4-bit operators refuse, and their sizes, on the CPU: every call here
 returns before any GPU work (no pointer is read)."""
-import ctypes
+import struct
 
 import pytest
 
@@ -10,7 +10,7 @@ P = 1 << 20  # an address that is never read
 
 
 def _h(p=P, seq=8, token=8, head=8):
-    return vb.vla_heads(p, seq, token, head)
+    return struct.pack("Pqqq", p or 0, seq, token, head)
 
 
 def _name(code):
