@@ -31,6 +31,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t ONES = 0x3f803f80u;  // bf16 1.0 twice
 constexpr int BLK = 32;  // tokens per block
 constexpr float RAISE = 8.f;  // log2 by which a weight may exceed 1
+constexpr float UNIT = 64.f;  // what a step is at most as fp16: with RAISE 2^14, which leaves the small weights the most bits
 constexpr int KROT = 3, VROT = 6;
 __host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
 
@@ -309,13 +310,14 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 //    keys) and two multiply-adds in fp32; sum q is a constant of the loop.
 //  * softmax: a running maximum and sum per query, in fp32, one pass.
 //  * values: with P the weights and per group P' = P s_g,
-//      sum P v = sum P' (16 + c) + sum P (m_g - 16 s_g)
-//    the first sum by MFMA, the second in fp32 in the lane that holds P.  P' is
-//    rounded to fp16, relative to a power of two at or above the largest s_g
-//    of the group so far (`unit` is its inverse), which keeps it in fp16's
-//    range whatever the values' size: 2^-12 of at most 31 s_g P a key, a fifth of
-//    a bf16 result's own rounding.  (bf16 would be twice that rounding; hi and lo
-//    bf16 parts cost 12 instructions a row and group against 5.)
+//      sum P v = sum P' (16 + c) - 16 sum P' + sum P m_g
+//    the first sum by MFMA, the others in fp32 in the lane that holds P.  P' is
+//    rounded to fp16, in units of a 64th of the power of two above the largest
+//    s_g of the group so far (`unit` is the inverse), which keeps it in
+//    fp16's range whatever the values' size.  16 sum P' is of the rounded P', so
+//    that rounding costs 2^-12 of at most 15 s_g P a key, a quarter of a bf16
+//    result's own rounding.  (In bf16 it would be twice that rounding; hi and lo
+//    bf16 parts cost 12 instructions a row and group against 6.)
 // The 4 R queries of a tile sit in the MFMA rows 4 i + r, r < R, so with up to
 // four of them a lane holds one useful score a key and not four (R = 1).
 // P crosses from score lanes (one key each) to operand lanes (8 keys of one
@@ -392,7 +394,7 @@ __device__ __forceinline__ void store_row(const Kv4Attn& a, int b, int hk, int g
 }
 
 template <int DH, int R, int W>
-__global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
+__global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(Kv4Attn a) {
   constexpr int NG = DH / 32, ND = DH / 16, RT = 4 * R;
   // P' of a wave [group][query][32 keys] while it runs, then its output [query][DH]
   constexpr int PW = NG * RT * 16, OW = RT * DH;  // words
@@ -479,7 +481,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zero;
-  float m[R], l[R], bias[R][NG], unit[NG];
+  float m[R], l[R], bias[R][NG], psum[R][NG], unit[NG];  // sums of P, P m and P' of this lane's keys
 #pragma unroll
   for (int g = 0; g < NG; ++g) unit[g] = 0x1p126f;  // every step but 0 exceeds it
 #pragma unroll
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     m[r] = -INFINITY;
     l[r] = 0.f;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) bias[r][g] = 0.f;
+    for (int g = 0; g < NG; ++g) bias[r][g] = psum[r][g] = 0.f;
   }
   for (int j = j0 + wave; j < j1; j += W) {
     const int key0 = block_of(j) * BLK;
@@ -526,7 +528,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
           p[t][r] = (key <= last[r]) & ((key >= first[r]) | (key < a.sinks)) ? p[t][r] : -INFINITY;
         }
     }
-    float vs[2][NG], vm[2][NG], steps[2][NG];
+    float vs[2][NG], steps[2][NG];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int key = key0 + t * 16 + c16;
@@ -534,9 +536,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
       const bool seen = whole || ((key <= sn.pos1) & (!a.window | (key > sn.pos0 - a.window) | (key < a.sinks)));
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const float s = lo16(vp[t].w[g]);
-        vm[t][g] = fmaf(-16.f, s, hi16(vp[t].w[g]));
-        steps[t][g] = seen ? s : 0.f;
+        steps[t][g] = seen ? lo16(vp[t].w[g]) : 0.f;
         vs[t][g] = steps[t][g] * unit[g];
       }
     }
@@ -553,13 +553,13 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     float most = fmaxf(vs[0][0], vs[1][0]);
 #pragma unroll
     for (int g = 1; g < NG; ++g) most = fmaxf(most, fmaxf(vs[0][g], vs[1][g]));
-    if (__any(raise || most > 1.f)) {
+    if (__any(raise || most > UNIT)) {
       float f[NG];  // what the group's unit changes by
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        // 1 / unit: the power of two above the largest step so far
+        // UNIT / unit: the power of two above the largest step so far
         const uint32_t e = __float_as_uint(row_max<>(fmaxf(steps[0][g], steps[1][g]))) & 0x7f800000u;
-        const float u = fminf(unit[g], e && e < 0x7f800000u ? __uint_as_float(0x7e800000u - e) : 0x1p126f);
+        const float u = fminf(unit[g], e && e < 0x7f800000u ? UNIT * __uint_as_float(0x7e800000u - e) : 0x1p126f);
         f[g] = u * inverse2(unit[g]);
         unit[g] = u;
         vs[0][g] = steps[0][g] * u;
@@ -572,7 +572,10 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
         m[r] = mn;
         l[r] *= al;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) bias[r][g] *= al;
+        for (int g = 0; g < NG; ++g) {
+          bias[r][g] *= al;
+          psum[r][g] *= al * f[g];
+        }
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d][r] *= al * f[d / 2];
       }
@@ -587,14 +590,16 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of pw come first
     __builtin_amdgcn_wave_barrier();
     auto put = [&](int g, int r, float p0, float p1) {
-      pw[(g * RT + kq * R + r) * 16 + c16] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), f16x2));
+      const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
+      psum[r][g] = __builtin_amdgcn_fdot2(h, f16x2{(_Float16)1.f, (_Float16)1.f}, psum[r][g], false);
+      pw[(g * RT + kq * R + r) * 16 + c16] = __builtin_bit_cast(uint32_t, h);
     };
     if (whole) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          bias[r][g] = fmaf(p[0][r], vm[0][g], fmaf(p[1][r], vm[1][g], bias[r][g]));
+          bias[r][g] = fmaf(p[0][r], hi16(vp[0].w[g]), fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]));
           put(g, r, p[0][r] * vs[0][g], p[1][r] * vs[1][g]);
         }
     } else {  // a key that the row does not see may hold NaN
@@ -603,8 +608,8 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
         const bool s0 = p[0][r] != 0.f, s1 = p[1][r] != 0.f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float b1 = s1 ? fmaf(p[1][r], vm[1][g], bias[r][g]) : bias[r][g];
-          bias[r][g] = s0 ? fmaf(p[0][r], vm[0][g], b1) : b1;
+          const float b1 = s1 ? fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]) : bias[r][g];
+          bias[r][g] = s0 ? fmaf(p[0][r], hi16(vp[0].w[g]), b1) : b1;
           put(g, r, s0 ? p[0][r] * vs[0][g] : 0.f, s1 ? p[1][r] * vs[1][g] : 0.f);
         }
       }
@@ -633,7 +638,7 @@ __global__ __launch_bounds__(W * 64) void kv4_attention_kernel(Kv4Attn a) {
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float bs = row_sum<>(bias[r][g]), w = inverse2(unit[g]);
+      const float w = inverse2(unit[g]), bs = row_sum<>(fmaf(-16.f * psum[r][g], w, bias[r][g]));
 #pragma unroll
       for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = fmaf(o[d][r], w, bs);
     }
@@ -727,10 +732,10 @@ struct Plan {
 // in tenths of a microsecond: a wave alone on its SIMD takes 1.8 a block, a
 // SIMD 0.8 a block and 0.8 more a wave, whatever R and dh (memory latency and
 // the LDS round trip weigh more than instructions); one CU takes the
-// workgroups past 256; joining splits costs 5, and 0.5 more past every 16
-// splits.  Over 31 calls timed at every choice (1 to 64 sequences, 1 to 131072
-// tokens, R = 1, 2, 4, windows), 17 choices each, what this takes is 0.06%
-// slower than the fastest on average and 1% at most; a fixed aim of 1024
+// workgroups past 256; joining splits costs 3.5, and 0.5 more past every 16
+// splits.  Over 46 calls timed at every choice (1 to 64 sequences, 1 to 131072
+// tokens, R = 1, 2, 4, windows), up to 34 choices each, what this takes is
+// 0.2% slower than the fastest on average and 3% at most; a fixed aim of 1024
 // workgroups of four waves lost up to 40%.
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
@@ -751,7 +756,7 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
       if (per > most) per = most;
       const int64_t ns = (blocks + per * W - 1) / (per * W);
       const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 18 * per, simd = a_simd * (8 * per + 8);
-      const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 50 + 5 * ((ns - 1) / 16) : 0);
+      const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 35 + 5 * ((ns - 1) / 16) : 0);
       if (cost < best && ns <= 4096) best = cost, p.W = W, p.chunk = (int)(per * W), p.nsplit = (int)ns;
       if (per == most) break;
     }
