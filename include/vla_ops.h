@@ -120,8 +120,10 @@ vla_status vla_op_w4_pack(const void *codes, const void *scales, const void *zer
  * few rows of a decode step (the weights are read once per 16 rows).
  * swiglu: W holds N / 2 gate rows, then the N / 2 up rows, and out[M][N / 2] =
  * silu(x Wgate^T) * (x Wup^T) + residual; N % 32 == 0.
- * Row strides in elements: ldx of x (a multiple of 8; x 16-byte aligned), ldo
- * of out and of residual, which may be the same memory (fp32 out). */
+ * Row strides in elements, no less than a row's width where M > 1: ldx of x (a
+ * multiple of 8; x 16-byte aligned), ldo of out and of residual, which may be
+ * the same memory (fp32 out).  A row of x that is not finite gives a row of
+ * out that is not finite, and reaches no other row. */
 vla_status vla_op_gemv_w4(const void *x, int64_t ldx, const void *Wp, const float *residual, void *out, int64_t ldo,
                           vla_dtype out_dtype, int swiglu, int M, int N, int K, int group, void *stream);
 
@@ -133,7 +135,8 @@ vla_status vla_op_gemv_w4(const void *x, int64_t ldx, const void *Wp, const floa
  * gq[dh], gk[dh] fp32 gains, each NULL = no norm; cos, sin both NULL = no
  * rotation.  pos[B][L] (device int32), NULL = the token's index t; with
  * rotation, a token whose position is not in [0, n_pos) is padding: its rows
- * of q_out and k_out stay as they were.  Gains and tables 16-byte aligned.
+ * of q_out and k_out stay as they were.  Gains and tables 16-byte aligned,
+ * eps >= 0.
  * q_out and k_out may be q and k themselves (bf16, same strides).  dh in {64, 128}. */
 vla_status vla_op_qk_norm_rope(const vla_heads *q, const vla_heads *k, vla_dtype in_dtype, const float *gq,
                                const float *gk, float eps, const float *cos, const float *sin, int n_pos,

@@ -461,7 +461,7 @@ def _dense(t, dtype, shape, dev, what):
 
 def _memory(t, need, dev, what):
     """Address of at least `need` bytes of dense memory."""
-    if t.numel() * t.element_size() < need or t.get_device() != dev or not t.is_contiguous():
+    if t.nbytes < need or t.get_device() != dev or not t.is_contiguous():
         _bad("%s: %d contiguous bytes on the same GPU are needed" % (what, need))
     return t.data_ptr()
 
@@ -470,11 +470,12 @@ def _heads(t, dtype, shape, dev, what):
     """The vla_heads of a tensor [B, tokens, heads, dh] of any outer strides."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         _bad("%s: a %s tensor of shape %s on the same GPU is needed" % (what, dtype, tuple(shape)))
-    s = t.stride()
-    if s[3] != 1:
+    a, b, c, d = t.stride()
+    if d != 1:
         _bad("%s: the last dimension has to be dense" % what)
-    # the stride of a dimension of one is never used
-    return _HEADS(t.data_ptr(), s[0] if shape[0] != 1 else 0, s[1] if shape[1] != 1 else 0, s[2] if shape[2] != 1 else 0)
+    if (a | b | c) & 7:  # a dimension of one may have any stride; it is never used
+        a, b, c = (x if n != 1 else 0 for x, n in zip((a, b, c), shape))
+    return _HEADS(t.data_ptr(), a, b, c)
 
 
 def vla_op_w4_packed_bytes(N, K, group):
@@ -499,7 +500,7 @@ def vla_op_gemv_w4(x, Wp, residual, out, N, group, swiglu=False, stream=None):
     (float32 or bfloat16), rows of any stride; residual's rows and out's are
     equally far apart."""
     dev = _device(x, "x")
-    L = lib()
+    L = _lib or lib()
     if x.dtype is not _BF16 or x.dim() != 2 or x.stride(1) != 1:
         _bad("x: bfloat16 [M, K] with dense rows is needed")
     M, K = x.shape
@@ -514,8 +515,12 @@ def vla_op_gemv_w4(x, Wp, residual, out, N, group, swiglu=False, stream=None):
                 or residual.get_device() != dev or (M > 1 and residual.stride(0) != ldo)):
             _bad("residual: float32 %s with out's row stride on the same GPU is needed" % (wide,))
         res = residual.data_ptr()
-    code = L.vla_op_gemv_w4(x.data_ptr(), ldx, _memory(Wp, L.vla_op_w4_packed_bytes(N, K, group), dev, "Wp"), res,
-                            out.data_ptr(), ldo, f32, bool(swiglu), M, N, K, group, stream)
+    if group <= 0:
+        _bad("group: a positive size is needed")
+    # vla_op_w4_packed_bytes
+    need = (N + 15 >> 4) * (K + 127 >> 7) * (1024 + 64 * (128 // group))
+    code = L.vla_op_gemv_w4(x.data_ptr(), ldx, _memory(Wp, need, dev, "Wp"), res, out.data_ptr(), ldo, f32, bool(swiglu), M,
+                            N, K, group, stream)
     if code:
         _check(code)
 
@@ -532,7 +537,7 @@ def vla_op_qk_norm_rope(q, k, gq, gk, eps, cos, sin, pos, q_out, k_out, stream=N
     B, L, H, dh = qs
     ks = (B, L, ks[2], dh)
     n_pos = 0 if cos is None else cos.shape[0]
-    code = lib().vla_op_qk_norm_rope(
+    code = (_lib or lib()).vla_op_qk_norm_rope(
         _heads(q, dt, qs, dev, "q"), _heads(k, dt, ks, dev, "k"), dt is _F32, _dense(gq, _F32, (dh,), dev, "gq"),
         _dense(gk, _F32, (dh,), dev, "gk"), eps, _dense(cos, _F32, (n_pos, dh // 2), dev, "cos"),
         _dense(sin, _F32, (n_pos, dh // 2), dev, "sin"), n_pos, _dense(pos, _I32, (B, L), dev, "pos"),
@@ -545,18 +550,23 @@ def vla_op_kv4_bytes(B, Hkv, L_cap, dh):
     return lib().vla_op_kv4_bytes(B, Hkv, L_cap, dh)
 
 
+def _kv4_bytes(B, Hkv, L_cap, dh):
+    """vla_op_kv4_bytes of sizes that it takes, without the call."""
+    return B * Hkv * (L_cap >> 5) * 40 * dh
+
+
 def vla_op_kv4_store(k, v, start, count, cache, L_cap, stream=None):
     """k, v [B, L, Hkv, dh] bfloat16, start, count [B] int32 or None, cache a
     tensor of vla_op_kv4_bytes(B, Hkv, L_cap, dh) bytes."""
     dev = _device(k, "k")
-    L = lib()
+    L = _lib or lib()
     shape = k.shape
     if len(shape) != 4:
         _bad("k: [B, L, Hkv, dh] is needed")
     B, n, Hkv, dh = shape
     code = L.vla_op_kv4_store(
         _heads(k, _BF16, shape, dev, "k"), _heads(v, _BF16, shape, dev, "v"), _dense(start, _I32, (B,), dev, "start"),
-        _dense(count, _I32, (B,), dev, "count"), _memory(cache, L.vla_op_kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), B,
+        _dense(count, _I32, (B,), dev, "count"), _memory(cache, _kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), B,
         n, Hkv, L_cap, dh, stream)
     if code:
         _check(code)
@@ -565,13 +575,13 @@ def vla_op_kv4_store(k, v, start, count, cache, L_cap, stream=None):
 def vla_op_kv4_load(cache, L_cap, start, count, k, v, stream=None):
     """The inverse of vla_op_kv4_store, into k and v."""
     dev = _device(k, "k")
-    L = lib()
+    L = _lib or lib()
     shape = k.shape
     if len(shape) != 4:
         _bad("k: [B, L, Hkv, dh] is needed")
     B, n, Hkv, dh = shape
     code = L.vla_op_kv4_load(
-        _memory(cache, L.vla_op_kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), _dense(start, _I32, (B,), dev, "start"),
+        _memory(cache, _kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), _dense(start, _I32, (B,), dev, "start"),
         _dense(count, _I32, (B,), dev, "count"), _heads(k, _BF16, shape, dev, "k"), _heads(v, _BF16, shape, dev, "v"), B,
         n, Hkv, L_cap, dh, stream)
     if code:
@@ -586,14 +596,14 @@ def vla_op_attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window=0, sinks
     """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a tensor of
     vla_op_attention_kv4_scratch(...) bytes (None where that is 0)."""
     dev = _device(q, "q")
-    L = lib()
+    L = _lib or lib()
     shape = q.shape
     if len(shape) != 4 or lens is None:
         _bad("q [B, Lq, H, dh] and lens [B] are needed")
     B, Lq, H, dh = shape
-    nbytes = 0 if scratch is None else scratch.numel() * scratch.element_size()
+    nbytes = 0 if scratch is None else scratch.nbytes
     code = L.vla_op_attention_kv4(
-        _heads(q, _BF16, shape, dev, "q"), _memory(cache, L.vla_op_kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"),
+        _heads(q, _BF16, shape, dev, "q"), _memory(cache, _kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"),
         _dense(lens, _I32, (B,), dev, "lens"), _heads(o, _BF16, shape, dev, "o"), B, Lq, H, Hkv, L_cap, dh, max_len,
         window, sinks, _memory(scratch, nbytes, dev, "scratch") if nbytes else None, nbytes, stream)
     if code:

@@ -15,7 +15,8 @@ static_assert((int)vla::GemmOp::F32 == VLA_GEMM_F32 && (int)vla::GemmOp::RESIDUA
               "vla_gemm_op names GemmOp's values");
 
 // ---- checks of the 4-bit operators' arguments
-constexpr int64_t MAX_GRID = 0x3fffffff;  // workgroups, rows of a call
+// a launch has fewer than 2^32 threads along x: 2 x 256 (cache rows), 512 or 256 a unit below
+constexpr int64_t MAX_GRID = 0x7fffff;
 bool aligned(const void* p, uintptr_t n) { return (uintptr_t)p % n == 0; }
 bool readable(const vla_heads& h, int B, int L) {
   return (h.p || B == 0 || L == 0) && h.seq >= 0 && h.token >= 0 && h.head >= 0;
@@ -30,7 +31,7 @@ vla::Heads heads(const vla_heads& h) { return {h.p, h.seq, h.token, h.head}; }
 vla_status w4_check(int N, int K, int group) {
   if (N <= 0 || K <= 0) return VLA_ERR_INVALID_ARG;
   if (K % 8 || (group != 32 && group != 64 && group != 128)) return VLA_ERR_UNSUPPORTED;
-  if (N > MAX_GRID || K > MAX_GRID) return VLA_ERR_UNSUPPORTED;
+  if (N > 1 << 25 || K > 1 << 25) return VLA_ERR_UNSUPPORTED;
   return VLA_OK;
 }
 
@@ -59,7 +60,7 @@ vla_status kv4_rows(const vla_heads* k, const vla_heads* v, const int32_t* start
 vla_status attn_check(int B, int Lq, int H, int Hkv, int dh, int max_len, int* window, int* sinks) {
   if (B < 0 || Lq < 0 || H <= 0 || Hkv <= 0 || max_len < 0 || *window < 0 || *sinks < 0) return VLA_ERR_INVALID_ARG;
   if (H % Hkv || (dh != 64 && dh != 128) || max_len > 1 << 24 || (int64_t)Lq * H > MAX_GRID ||
-      (int64_t)B * Lq * H > MAX_GRID)
+      (int64_t)B * Lq * H > MAX_GRID || (int64_t)B * Hkv > MAX_GRID)
     return VLA_ERR_UNSUPPORTED;
   if (*window >= max_len) *window = 0;
   if (*sinks > max_len) *sinks = max_len;
@@ -186,7 +187,7 @@ vla_status vla_op_qk_norm_rope(const vla_heads* q, const vla_heads* k, vla_dtype
                                const float* gk, float eps, const float* cos, const float* sin, int n_pos,
                                const int32_t* pos, const vla_heads* q_out, const vla_heads* k_out, int B, int L, int H,
                                int Hkv, int dh, void* stream) {
-  if (!q || !k || !q_out || !k_out || !cos != !sin || n_pos < 0 || B < 0 || L < 0 || H <= 0 || Hkv <= 0 ||
+  if (!q || !k || !q_out || !k_out || !cos != !sin || !(eps >= 0.f) || n_pos < 0 || B < 0 || L < 0 || H <= 0 || Hkv <= 0 ||
       (in_dtype != VLA_BF16 && in_dtype != VLA_F32) || !readable(*q, B, L) || !readable(*k, B, L) ||
       !writable(*q_out, B, L, H) || !writable(*k_out, B, L, Hkv))
     return VLA_ERR_INVALID_ARG;

@@ -303,6 +303,24 @@ def test_attention_strides_streams_and_graph():
         _check(got, q, k, v, lens, 0, 0)
 
 
+def test_offsets_past_32_bits():
+    """Two heads of 2^24 tokens (5.4 GB): rows at the far end of the second
+    come back, and a window there is attended to."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    B, H, Hkv, dh, cap, n = 1, 4, 2, 128, 1 << 24, 70
+    k, v = _kv(("far",), B, n, Hkv, dh)
+    q = ref.normal(("farq",), (B, 1, H, dh))
+    cache = torch.empty(vb.vla_op_kv4_bytes(B, Hkv, cap, dh), dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 1 << 32
+    vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(v), _i32(cap - n), None, cache, cap)
+    got = _load(cache, cap, B, n, Hkv, dh, _i32(cap - n))
+    assert np.array_equal(got[0], ref.bf16(ref.cached(k))) and np.array_equal(got[1], ref.bf16(ref.cached(v)))
+    out = _attend(ref.to_dev(q), cache, cap, Hkv, [cap], cap, 60, 0)
+    # the last 60 of these tokens, as a sequence of their own
+    _check(out, q, k, v, [n], 60, 0)
+
+
 def test_batch_does_not_change_a_sequence():
     """A sequence's cache and result are the same bytes next to other sequences,
     where both calls split the keys alike."""

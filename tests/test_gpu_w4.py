@@ -106,6 +106,25 @@ def test_gemv_w4_swiglu(M, F, K, group, f32):
     assert (np.abs(ref.from_dev(out) - want) <= bound + 1e-30).all()
 
 
+def test_gemv_w4_swiglu_and_residual():
+    """The gated product on top of a residual, in place in fp32."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    M, F, K, group = 5, 80, 192, 64
+    codes, s, z = _weights((M, F, K, group), 2 * F, K, group, True, False)
+    x = ref.normal(("w4x", M, K), (M, K))
+    y = x @ ref.w4_weights(codes, s, z, group).T
+    b, _ = _bound(x, codes, s, z, group)
+    g, u = y[:, :F], y[:, F:]
+    h0 = synth.normal_f32(synth.seed_of("w4sh", M, F), (M, F))
+    h = torch.from_numpy(h0.copy()).cuda()
+    vb.vla_op_gemv_w4(ref.to_dev(x), _packed(codes, s, z, group), h, h, 2 * F, group, True)
+    sg = g / (1 + np.exp(-g))
+    want = h0 + sg * u
+    bound = 1.1 * b[:, :F] * (np.abs(u) + b[:, F:]) + np.abs(sg) * b[:, F:] + 2.0 ** -20 * np.abs(sg * u) + 2.0 ** -23 * (np.abs(want) + np.abs(h0))
+    assert (np.abs(ref.from_dev(h) - want) <= bound).all()
+
+
 def test_gemv_w4_strides_and_neighbours():
     """Rows of x inside a wider array, rows of out with a tail that stays as it
     was, and a row of x that is not finite: it reaches no other row."""

@@ -28,7 +28,7 @@ GEMV = dict(x=P, ldx=256, Wp=P, residual=None, out=P, ldo=64, out_dtype=vb.VLA_F
     (dict(K=252, ldx=256), "UNSUPPORTED"), (dict(group=16), "UNSUPPORTED"), (dict(group=0), "UNSUPPORTED"),
     (dict(group=256), "UNSUPPORTED"), (dict(ldx=260), "UNSUPPORTED"), (dict(x=P + 8), "UNSUPPORTED"),
     (dict(Wp=P + 4), "UNSUPPORTED"), (dict(out=P + 2), "UNSUPPORTED"), (dict(residual=P + 1), "UNSUPPORTED"),
-    (dict(swiglu=1, N=48), "UNSUPPORTED"), (dict(M=16 * 65535 + 1), "UNSUPPORTED")])
+    (dict(swiglu=1, N=48), "UNSUPPORTED"), (dict(N=(1 << 25) + 1, ldo=1 << 26), "UNSUPPORTED"), (dict(ldx=1 << 30), "UNSUPPORTED"), (dict(M=16 * 65535 + 1), "UNSUPPORTED")])
 def test_gemv_w4_refuses(change, code):
     assert _name(vb.lib().vla_op_gemv_w4(*{**GEMV, **change}.values())) == "VLA_ERR_" + code
 
@@ -81,6 +81,7 @@ QK = dict(q=_h(), k=_h(), dt=vb.VLA_BF16, gq=P, gk=P, eps=1e-6, cos=P, sin=P, n_
     (dict(q=None), "INVALID_ARG"), (dict(ko=None), "INVALID_ARG"), (dict(q=_h(None)), "INVALID_ARG"),
     (dict(cos=None), "INVALID_ARG"), (dict(sin=None), "INVALID_ARG"), (dict(n_pos=-1), "INVALID_ARG"),
     (dict(B=-1), "INVALID_ARG"), (dict(H=0), "INVALID_ARG"), (dict(Hkv=0), "INVALID_ARG"), (dict(dt=5), "INVALID_ARG"),
+    (dict(eps=-1e-6), "INVALID_ARG"), (dict(eps=float("nan")), "INVALID_ARG"),
     (dict(q=_h(seq=-8)), "INVALID_ARG"), (dict(qo=_h(token=0)), "INVALID_ARG"), (dict(ko=_h(head=0)), "INVALID_ARG"),
     (dict(dh=96), "UNSUPPORTED"), (dict(q=_h(P + 2)), "UNSUPPORTED"), (dict(ko=_h(head=4)), "UNSUPPORTED"),
     (dict(gq=P + 4), "UNSUPPORTED"), (dict(sin=P + 8), "UNSUPPORTED"), (dict(pos=P + 2), "UNSUPPORTED"),
@@ -123,7 +124,7 @@ ATT = dict(q=_h(), cache=P, lens=P, o=_h(), B=1, Lq=1, H=4, Hkv=2, L_cap=4096, d
     (dict(scratch=None), "INVALID_ARG"), (dict(o=_h(head=0)), "INVALID_ARG"), (dict(q=_h(head=-8)), "INVALID_ARG"),
     (dict(H=5), "UNSUPPORTED"), (dict(dh=256), "UNSUPPORTED"), (dict(L_cap=4097), "UNSUPPORTED"),
     (dict(q=_h(P + 4)), "UNSUPPORTED"), (dict(o=_h(seq=4)), "UNSUPPORTED"), (dict(scratch=P + 4), "UNSUPPORTED"),
-    (dict(cache=P + 2), "UNSUPPORTED"), (dict(max_len=4097), "SHAPE"), (dict(nbytes=4), "SHAPE"),
+    (dict(cache=P + 2), "UNSUPPORTED"), (dict(B=1 << 20, H=64, Hkv=32), "UNSUPPORTED"), (dict(Lq=1 << 30), "UNSUPPORTED"), (dict(max_len=4097), "SHAPE"), (dict(nbytes=4), "SHAPE"),
     (dict(scratch=None, nbytes=0), "SHAPE")])
 def test_attention_kv4_refuses(change, code):
     assert _name(vb.lib().vla_op_attention_kv4(*{**ATT, **change}.values())) == "VLA_ERR_" + code
