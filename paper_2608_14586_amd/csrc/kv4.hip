@@ -30,6 +30,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t ONES = 0x3f803f80u;  // bf16 1.0 twice
 constexpr int BLK = 32;  // tokens per block
+constexpr float LOWEST = -3e38f;  // a maximum before any score: finite, so that no difference of two is NaN
 constexpr float RAISE = 8.f;  // log2 by which a weight may exceed 1
 constexpr float UNIT = 64.f;  // what a step is at most as fp16: with RAISE 2^14, which leaves the small weights the most bits
 constexpr int KROT = 3, VROT = 6;
@@ -486,7 +487,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   for (int g = 0; g < NG; ++g) unit[g] = 0x1p126f;  // every step but 0 exceeds it
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    m[r] = -INFINITY;
+    m[r] = LOWEST;
     l[r] = 0.f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) bias[r][g] = psum[r][g] = 0.f;
@@ -514,42 +515,33 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
       for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int r = 0; r < R; ++r) p[t][r] = fmaf(lo16(kp[t].w[g]), d[g][r], p[t][r]);
-#pragma unroll
-      for (int r = 0; r < R; ++r) p[t][r] *= a.scale_log2;
     }
     if (j + W < j1) fetch_keys(j + W);
     if (!whole) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const int key = key0 + t * 16 + c16;
+        // also replaces whatever the cache's unwritten rows gave
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const int key = key0 + t * 16 + c16;
-          // also replaces whatever the cache's unwritten rows gave
+        for (int r = 0; r < R; ++r)
           p[t][r] = (key <= last[r]) & ((key >= first[r]) | (key < a.sinks)) ? p[t][r] : -INFINITY;
-        }
-    }
-    float vs[2][NG], steps[2][NG];
+        // what a row that nobody sees holds must not choose the unit: its step becomes 0
+        const bool seen = (key <= sn.pos1) & (!a.window | (key > sn.pos0 - a.window) | (key < a.sinks));
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int key = key0 + t * 16 + c16;
-      // what a row that nobody sees holds must not choose the unit
-      const bool seen = whole || ((key <= sn.pos1) & (!a.window | (key > sn.pos0 - a.window) | (key < a.sinks)));
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        steps[t][g] = seen ? lo16(vp[t].w[g]) : 0.f;
-        vs[t][g] = steps[t][g] * unit[g];
+        for (int g = 0; g < NG; ++g) vp[t].w[g] &= seen ? 0xffffffffu : 0xffff0000u;
       }
     }
+    float vs[2][NG];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) vs[t][g] = lo16(vp[t].w[g]) * unit[g];
     // the running maximum moves only where a score exceeds it by RAISE, and
     // the unit of a group's steps only where a step exceeds it, so most blocks
-    // rescale nothing
-    float up[R];
+    // rescale nothing, and a lane asks for its own keys alone
     bool raise = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      up[r] = row_max<>(fmaxf(p[0][r], p[1][r]));
-      raise |= up[r] > m[r] + RAISE;
-    }
+    for (int r = 0; r < R; ++r) raise |= fmaxf(p[0][r], p[1][r]) * a.scale_log2 > m[r] + RAISE;
     float most = fmaxf(vs[0][0], vs[1][0]);
 #pragma unroll
     for (int g = 1; g < NG; ++g) most = fmaxf(most, fmaxf(vs[0][g], vs[1][g]));
@@ -558,17 +550,18 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         // UNIT / unit: the power of two above the largest step so far
-        const uint32_t e = __float_as_uint(row_max<>(fmaxf(steps[0][g], steps[1][g]))) & 0x7f800000u;
+        const float s0 = lo16(vp[0].w[g]), s1 = lo16(vp[1].w[g]);
+        const uint32_t e = __float_as_uint(row_max<>(fmaxf(s0, s1))) & 0x7f800000u;
         const float u = fminf(unit[g], e && e < 0x7f800000u ? UNIT * __uint_as_float(0x7e800000u - e) : 0x1p126f);
         f[g] = u * inverse2(unit[g]);
         unit[g] = u;
-        vs[0][g] = steps[0][g] * u;
-        vs[1][g] = steps[1][g] * u;
+        vs[0][g] = s0 * u;
+        vs[1][g] = s1 * u;
       }
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const float mn = fmaxf(m[r], up[r]);
-        const float al = mn == -INFINITY ? 1.f : exp2_of(m[r] - mn);
+        const float mn = fmaxf(m[r], row_max<>(fmaxf(p[0][r], p[1][r])) * a.scale_log2);
+        const float al = exp2_of(m[r] - mn);
         m[r] = mn;
         l[r] *= al;
 #pragma unroll
@@ -582,9 +575,8 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const float ms = m[r] == -INFINITY ? 0.f : m[r];
-      p[0][r] = exp2_of(p[0][r] - ms);
-      p[1][r] = exp2_of(p[1][r] - ms);
+      p[0][r] = exp2_of(fmaf(p[0][r], a.scale_log2, -m[r]));
+      p[1][r] = exp2_of(fmaf(p[1][r], a.scale_log2, -m[r]));
       l[r] += p[0][r] + p[1][r];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of pw come first
@@ -654,7 +646,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     f32x4 v = zero;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float f = sm[w][row] == -INFINITY ? 0.f : exp2_of(sm[w][row] - mx);
+      const float f = exp2_of(sm[w][row] - mx);
       ls = fmaf(f, sl[w][row], ls);
       const f32x4 x = *(const f32x4*)((const float*)lds[w] + row * DH + d);
 #pragma unroll
@@ -695,14 +687,14 @@ __global__ __launch_bounds__(64) void kv4_combine_kernel(Kv4Attn a, int total) {
   const int row0 = gr / RT * RT;
   const Seen sn = seen_of(a, min(max(length, 0), a.max_len), row0, min(rows, row0 + RT) - 1);
   const int ns = div_by(sn.nb + a.chunk - 1, a.by_chunk);
-  float mx = -INFINITY, l = 0.f;
+  float mx = LOWEST, l = 0.f;
   vec v = {};
   for (int s0 = 0; s0 < ns; s0 += 64) {
     if (s0) x = ml[min(s0 + lane, ns - 1)];
-    const float m = s0 + lane < ns ? x[0] : -INFINITY, mn = fmaxf(mx, wave_max(m));
-    const float f0 = mx == -INFINITY ? 0.f : exp2_of(mx - mn);
-    const float f = m == -INFINITY ? 0.f : exp2_of(m - mn);
-    l = fmaf(l, f0, wave_sum(m == -INFINITY ? 0.f : f * x[1]));
+    const bool there = s0 + lane < ns;
+    const float m = there ? x[0] : LOWEST, mn = fmaxf(mx, wave_max(m));
+    const float f0 = exp2_of(mx - mn), f = exp2_of(m - mn);
+    l = fmaf(l, f0, wave_sum(there ? f * x[1] : 0.f));
     v *= f0;
     mx = mn;
     const int n = min(64, ns - s0);
@@ -728,37 +720,44 @@ __global__ __launch_bounds__(64) void kv4_combine_kernel(Kv4Attn a, int total) {
 struct Plan {
   int R, W, tiles, chunk, nsplit;
 };
-// Waves a workgroup and blocks a wave, by the estimated time of each choice,
-// in tenths of a microsecond: a wave alone on its SIMD takes 1.8 a block, a
-// SIMD 0.8 a block and 0.8 more a wave, whatever R and dh (memory latency and
-// the LDS round trip weigh more than instructions); one CU takes the
-// workgroups past 256; joining splits costs 3.5, and 0.5 more past every 16
-// splits.  Over 46 calls timed at every choice (1 to 64 sequences, 1 to 131072
-// tokens, R = 1, 2, 4, windows), up to 34 choices each, what this takes is
-// 0.2% slower than the fastest on average and 3% at most; a fixed aim of 1024
-// workgroups of four waves lost up to 40%.
+// Queries a tile (4 R), waves a workgroup and blocks a wave, by the estimated
+// time of each choice, in hundredths of a microsecond: a wave alone on its SIMD
+// takes 180 a block, a SIMD 80 a block and 80 more a wave, 13% and 45% more
+// with R = 2 and 4 (memory latency and the LDS round trip weigh more than
+// instructions; dh hardly shows), and a launch 60 and 180 more; one CU takes
+// the workgroups past 256; joining splits costs 350, and 50 more past every 16
+// splits.  Over 46 calls timed at every choice of the last two (1 to 64
+// sequences, 1 to 131072 tokens, R = 1, 2, 4, windows), up to 34 each, what
+// this takes is 0.2% slower than the fastest on average and 3% at most; a fixed
+// aim of 1024 workgroups of four waves lost up to 40%.  Smaller tiles than the
+// queries need unpack the cache again for each, but where whole ones leave CUs
+// idle they are faster: 16 sequences of 12 queries over 8 heads and a window of
+// 1024, one tile 14.3 us, two 11.0.
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
-  Plan p;
-  p.R = rows <= 4 ? 1 : rows <= 8 ? 2 : 4;
-  p.tiles = (rows + 4 * p.R - 1) / (4 * p.R);
+  Plan p{};
   int64_t blocks = cdiv(max_len, BLK);
   if (window > 0) {
     const int64_t w = ((int64_t)window + Lq - 1 + BLK - 1) / BLK + 1 + cdiv(sinks, BLK);
     if (w < blocks) blocks = w;
   }
   if (blocks < 1) blocks = 1;
-  const int64_t bt = (int64_t)B * Hkv * p.tiles;
   int64_t best = INT64_MAX;
-  for (int W = 4; W <= 8; W += 4) {
-    const int64_t most = (blocks + W - 1) / W;
-    for (int64_t per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
-      if (per > most) per = most;
-      const int64_t ns = (blocks + per * W - 1) / (per * W);
-      const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 18 * per, simd = a_simd * (8 * per + 8);
-      const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 35 + 5 * ((ns - 1) / 16) : 0);
-      if (cost < best && ns <= 4096) best = cost, p.W = W, p.chunk = (int)(per * W), p.nsplit = (int)ns;
-      if (per == most) break;
+  for (int R = 1; R == 1 || (R <= 4 && 2 * R < rows); R *= 2) {
+    const int tiles = (rows + 4 * R - 1) / (4 * R);
+    const int64_t bt = (int64_t)B * Hkv * tiles;
+    const int64_t slower = R == 1 ? 100 : R == 2 ? 113 : 145, more = R == 1 ? 0 : R == 2 ? 60 : 180;
+    for (int W = 4; W <= 8; W += 4) {
+      const int64_t most = (blocks + W - 1) / W;
+      for (int64_t per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
+        if (per > most) per = most;
+        const int64_t ns = (blocks + per * W - 1) / (per * W);
+        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 180 * per, simd = a_simd * (80 * per + 80);
+        const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 350 + 50 * ((ns - 1) / 16) : 0);
+        if (cost < best && ns <= 4096 && tiles <= 65535)
+          best = cost, p = Plan{R, W, tiles, (int)(per * W), (int)ns};
+        if (per == most) break;
+      }
     }
   }
   return p;
@@ -825,7 +824,7 @@ size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len,
 
 hipError_t kv4_attention(Kv4Attn a, int dh, size_t scratch_bytes, hipStream_t s) {
   const Plan p = plan_of(a.B, a.Lq, a.H, a.Hkv, a.max_len, a.window, a.sinks);
-  if (p.tiles > 65535) return hipErrorInvalidValue;
+  if (!p.R) return hipErrorInvalidValue;  // more tiles than a grid has
   if (scratch_of(p, a.B, a.Lq, a.H, dh) > scratch_bytes) return hipErrorOutOfMemory;
   a.G = a.H / a.Hkv;
   a.by_G = fast_div(a.G);
