@@ -11,7 +11,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from ctypes import POINTER, c_char_p, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 import numpy as np
@@ -117,7 +116,7 @@ def lib():
             "vla_op_w4_pack": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
             "vla_op_gemv_w4": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int, c_int,
                                c_int, c_int, c_void_p],
-            # vla_heads go in as their 32 bytes
+            # a vla_heads goes in as its 32 bytes
             "vla_op_qk_norm_rope": [c_char_p, c_char_p, c_int, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_int,
                                     c_void_p, c_char_p, c_char_p, c_int, c_int, c_int, c_int, c_int, c_void_p],
             "vla_op_kv4_store": [c_char_p, c_char_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
@@ -415,67 +414,25 @@ def vla_op_gemm_tile_bf16(op, tile, A, Wp, out, bias, M, N, K, stream=None):
 
 # ----------------------------------------- 4-bit weights and KV cache (torch)
 # These calls take torch tensors on the GPU and read sizes and strides off
-# them; a tensor whose type, shape, device or size does not fit raises
-# ValueError before the library is called.  `stream`: a hipStream_t (torch's
-# `stream.cuda_stream`), None = the null stream.  A decode step's kernels take
-# two to five microseconds, so the checks are written to cost little: no
-# message is built and nothing converted unless something is wrong.
+# them (csrc/torch_ops.cpp); a tensor whose type, shape, device or size does
+# not fit raises ValueError before the library is called.  `stream`: a
+# hipStream_t (torch's `stream.cuda_stream`), None = the null stream.
 
-_HEADS = struct.Struct("Pqqq").pack  # a vla_heads
-_BF16 = _F32 = _I32 = None           # torch's types, once torch is there
-_current = None                      # the current device, where there are several
+_torch_ops = None
 
 
-def _types():
-    import torch
-    global _BF16, _F32, _I32, _current
-    _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
-    if torch.cuda.device_count() > 1:
-        _current = torch.cuda.current_device
-
-
-def _bad(what):
-    raise ValueError(what)
-
-
-def _device(t, what):
-    """Index of t's GPU, which has to be the current one (kernels run there)."""
-    d = t.get_device()
-    if _BF16 is None:
-        _types()
-    if d < 0:
-        _bad("%s: a tensor on the GPU is needed" % what)
-    if _current is not None and _current() != d:
-        _bad("%s: on device %d, which is not the current one" % (what, d))
-    return d
-
-
-def _dense(t, dtype, shape, dev, what):
-    """Address of a dense tensor of that type and shape (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-        _bad("%s: a contiguous %s tensor of shape %s on the same GPU is needed" % (what, dtype, tuple(shape)))
-    return t.data_ptr()
-
-
-def _memory(t, need, dev, what):
-    """Address of at least `need` bytes of dense memory."""
-    if t.nbytes < need or t.get_device() != dev or not t.is_contiguous():
-        _bad("%s: %d contiguous bytes on the same GPU are needed" % (what, need))
-    return t.data_ptr()
-
-
-def _heads(t, dtype, shape, dev, what):
-    """The vla_heads of a tensor [B, tokens, heads, dh] of any outer strides."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
-        _bad("%s: a %s tensor of shape %s on the same GPU is needed" % (what, dtype, tuple(shape)))
-    a, b, c, d = t.stride()
-    if d != 1:
-        _bad("%s: the last dimension has to be dense" % what)
-    if (a | b | c) & 7:  # a dimension of one may have any stride; it is never used
-        a, b, c = (x if n != 1 else 0 for x, n in zip((a, b, c), shape))
-    return _HEADS(t.data_ptr(), a, b, c)
+def _ops():
+    """The module of torch calls; raises if it has not been built."""
+    global _torch_ops
+    import torch  # noqa: F401  (its libraries come first)
+    lib()
+    try:
+        from . import _torch_ops as m
+    except ImportError as e:
+        raise RuntimeError("_torch_ops.so is missing or does not load (%s): build it with __graft_entry__.build() "
+                           "(there is no fallback)" % e)
+    _torch_ops = m
+    return m
 
 
 def vla_op_w4_packed_bytes(N, K, group):
@@ -485,42 +442,16 @@ def vla_op_w4_packed_bytes(N, K, group):
 def vla_op_w4_pack(codes, scales, zeros, Wp, group, stream=None):
     """codes [N, K] uint8, scales and zeros (or None) [N, ceil(K / group)]
     bfloat16 -> Wp, a tensor of vla_op_w4_packed_bytes(N, K, group) bytes."""
-    dev = _device(codes, "codes")
-    if codes.dim() != 2 or codes.element_size() != 1 or not codes.is_contiguous() or group <= 0:
-        _bad("codes: contiguous uint8 [N, K] and a group size are needed")
-    N, K = codes.shape
-    per = (N, -(-K // group))
-    _check(lib().vla_op_w4_pack(codes.data_ptr(), _dense(scales, _BF16, per, dev, "scales"),
-                                _dense(zeros, _BF16, per, dev, "zeros"),
-                                _memory(Wp, vla_op_w4_packed_bytes(N, K, group), dev, "Wp"), N, K, group, stream))
+    code = (_torch_ops or _ops()).w4_pack(codes, scales, zeros, Wp, group, stream)
+    if code:
+        _check(code)
 
 
 def vla_op_gemv_w4(x, Wp, residual, out, N, group, swiglu=False, stream=None):
     """x [M, K] bfloat16 and residual (None or float32), out [M, N or N / 2]
     (float32 or bfloat16), rows of any stride; residual's rows and out's are
     equally far apart."""
-    dev = _device(x, "x")
-    L = _lib or lib()
-    if x.dtype is not _BF16 or x.dim() != 2 or x.stride(1) != 1:
-        _bad("x: bfloat16 [M, K] with dense rows is needed")
-    M, K = x.shape
-    wide = (M, N // 2 if swiglu else N)
-    f32 = out.dtype is _F32
-    if not (f32 or out.dtype is _BF16) or out.shape != wide or out.stride(1) != 1 or out.get_device() != dev:
-        _bad("out: float32 or bfloat16 %s with dense rows on the same GPU is needed" % (wide,))
-    ldx, ldo = (x.stride(0), out.stride(0)) if M > 1 else (0, 0)
-    res = None
-    if residual is not None:
-        if (residual.dtype is not _F32 or residual.shape != wide or residual.stride(1) != 1
-                or residual.get_device() != dev or (M > 1 and residual.stride(0) != ldo)):
-            _bad("residual: float32 %s with out's row stride on the same GPU is needed" % (wide,))
-        res = residual.data_ptr()
-    if group <= 0:
-        _bad("group: a positive size is needed")
-    # vla_op_w4_packed_bytes
-    need = (N + 15 >> 4) * (K + 127 >> 7) * (1024 + 64 * (128 // group))
-    code = L.vla_op_gemv_w4(x.data_ptr(), ldx, _memory(Wp, need, dev, "Wp"), res, out.data_ptr(), ldo, f32, bool(swiglu), M,
-                            N, K, group, stream)
+    code = (_torch_ops or _ops()).gemv_w4(x, Wp, residual, out, N, group, swiglu, stream)
     if code:
         _check(code)
 
@@ -529,19 +460,7 @@ def vla_op_qk_norm_rope(q, k, gq, gk, eps, cos, sin, pos, q_out, k_out, stream=N
     """q, q_out [B, L, H, dh], k, k_out [B, L, Hkv, dh] (inputs bfloat16 or
     float32, outputs bfloat16), gq, gk [dh] and cos, sin [n_pos, dh / 2]
     float32 or None, pos [B, L] int32 or None."""
-    dev = _device(q, "q")
-    dt = q.dtype
-    qs, ks = q.shape, k.shape
-    if not (dt is _F32 or dt is _BF16) or len(qs) != 4 or len(ks) != 4:
-        _bad("q, k: float32 or bfloat16 [B, L, heads, dh] are needed")
-    B, L, H, dh = qs
-    ks = (B, L, ks[2], dh)
-    n_pos = 0 if cos is None else cos.shape[0]
-    code = (_lib or lib()).vla_op_qk_norm_rope(
-        _heads(q, dt, qs, dev, "q"), _heads(k, dt, ks, dev, "k"), dt is _F32, _dense(gq, _F32, (dh,), dev, "gq"),
-        _dense(gk, _F32, (dh,), dev, "gk"), eps, _dense(cos, _F32, (n_pos, dh // 2), dev, "cos"),
-        _dense(sin, _F32, (n_pos, dh // 2), dev, "sin"), n_pos, _dense(pos, _I32, (B, L), dev, "pos"),
-        _heads(q_out, _BF16, qs, dev, "q_out"), _heads(k_out, _BF16, ks, dev, "k_out"), B, L, H, ks[2], dh, stream)
+    code = (_torch_ops or _ops()).qk_norm_rope(q, k, gq, gk, eps, cos, sin, pos, q_out, k_out, stream)
     if code:
         _check(code)
 
@@ -550,40 +469,17 @@ def vla_op_kv4_bytes(B, Hkv, L_cap, dh):
     return lib().vla_op_kv4_bytes(B, Hkv, L_cap, dh)
 
 
-def _kv4_bytes(B, Hkv, L_cap, dh):
-    """vla_op_kv4_bytes of sizes that it takes, without the call."""
-    return B * Hkv * (L_cap >> 5) * 40 * dh
-
-
 def vla_op_kv4_store(k, v, start, count, cache, L_cap, stream=None):
     """k, v [B, L, Hkv, dh] bfloat16, start, count [B] int32 or None, cache a
     tensor of vla_op_kv4_bytes(B, Hkv, L_cap, dh) bytes."""
-    dev = _device(k, "k")
-    L = _lib or lib()
-    shape = k.shape
-    if len(shape) != 4:
-        _bad("k: [B, L, Hkv, dh] is needed")
-    B, n, Hkv, dh = shape
-    code = L.vla_op_kv4_store(
-        _heads(k, _BF16, shape, dev, "k"), _heads(v, _BF16, shape, dev, "v"), _dense(start, _I32, (B,), dev, "start"),
-        _dense(count, _I32, (B,), dev, "count"), _memory(cache, _kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), B,
-        n, Hkv, L_cap, dh, stream)
+    code = (_torch_ops or _ops()).kv4_store(k, v, start, count, cache, L_cap, stream)
     if code:
         _check(code)
 
 
 def vla_op_kv4_load(cache, L_cap, start, count, k, v, stream=None):
     """The inverse of vla_op_kv4_store, into k and v."""
-    dev = _device(k, "k")
-    L = _lib or lib()
-    shape = k.shape
-    if len(shape) != 4:
-        _bad("k: [B, L, Hkv, dh] is needed")
-    B, n, Hkv, dh = shape
-    code = L.vla_op_kv4_load(
-        _memory(cache, _kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"), _dense(start, _I32, (B,), dev, "start"),
-        _dense(count, _I32, (B,), dev, "count"), _heads(k, _BF16, shape, dev, "k"), _heads(v, _BF16, shape, dev, "v"), B,
-        n, Hkv, L_cap, dh, stream)
+    code = (_torch_ops or _ops()).kv4_load(k, v, start, count, cache, L_cap, stream)
     if code:
         _check(code)
 
@@ -595,17 +491,7 @@ def vla_op_attention_kv4_scratch(B, Lq, H, Hkv, dh, max_len, window=0, sinks=0):
 def vla_op_attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window=0, sinks=0, scratch=None, stream=None):
     """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a tensor of
     vla_op_attention_kv4_scratch(...) bytes (None where that is 0)."""
-    dev = _device(q, "q")
-    L = _lib or lib()
-    shape = q.shape
-    if len(shape) != 4 or lens is None:
-        _bad("q [B, Lq, H, dh] and lens [B] are needed")
-    B, Lq, H, dh = shape
-    nbytes = 0 if scratch is None else scratch.nbytes
-    code = L.vla_op_attention_kv4(
-        _heads(q, _BF16, shape, dev, "q"), _memory(cache, _kv4_bytes(B, Hkv, L_cap, dh), dev, "cache"),
-        _dense(lens, _I32, (B,), dev, "lens"), _heads(o, _BF16, shape, dev, "o"), B, Lq, H, Hkv, L_cap, dh, max_len,
-        window, sinks, _memory(scratch, nbytes, dev, "scratch") if nbytes else None, nbytes, stream)
+    code = (_torch_ops or _ops()).attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window, sinks, scratch, stream)
     if code:
         _check(code)
 

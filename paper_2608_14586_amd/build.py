@@ -1,16 +1,20 @@
 """Compile the HIP kernels and the C-ABI runtime into ``libvlaprefix.so``
-(gfx950 only) with hipcc.  Objects go to ``_build/`` next to this file."""
+(gfx950 only) with hipcc, and the binding's torch calls of the 4-bit operators
+into ``_torch_ops.so``.  Objects go to ``_build/`` next to this file."""
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libvlaprefix.so")
+TORCH_OPS = os.path.join(HERE, "_torch_ops.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -49,17 +53,41 @@ def _compile(src: str) -> str:
     return obj
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every source and link the shared library; returns its path."""
-    os.makedirs(OUT_DIR, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
-        objs = list(ex.map(_compile, SOURCES))
-    tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC", "-o", tmp] + objs
+def _torch_dir() -> str:
+    return list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+
+
+def _compile_torch_ops() -> str:
+    """Host code only: torch tensors in, calls of the C ABI out."""
+    obj = os.path.join(OUT_DIR, "torch_ops.cpp.o")
+    inc = os.path.join(_torch_dir(), "include")
+    cmd = ["g++", "-D__HIP_PLATFORM_AMD__"] + HOST_FLAGS + \
+        ["-I" + d for d in (inc, os.path.join(inc, "torch", "csrc", "api", "include"), "/opt/rocm/include",
+                            sysconfig.get_paths()["include"])] + ["-c", os.path.join(CSRC, "torch_ops.cpp"), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
+        raise RuntimeError("g++ failed for torch_ops.cpp:\n%s\n%s" % (" ".join(cmd), r.stderr[-6000:]))
+    return obj
+
+
+def _link(cmd, out: str) -> None:
+    tmp = out + ".tmp%d" % os.getpid()
+    r = subprocess.run(cmd + ["-o", tmp], capture_output=True, text=True)
+    if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (" ".join(cmd), r.stderr[-4000:]))
-    os.replace(tmp, LIB)
+    os.replace(tmp, out)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every source and link the shared library and the module of torch
+    calls; returns the library's path."""
+    os.makedirs(OUT_DIR, exist_ok=True)
+    with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as ex:
+        torch_obj = ex.submit(_compile_torch_ops)
+        objs = list(ex.map(_compile, SOURCES))
+    _link([HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC"] + objs, LIB)
+    _link(["g++", "-shared", torch_obj.result(), "-L" + HERE, "-lvlaprefix", "-Wl,-rpath,$ORIGIN",
+           "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], TORCH_OPS)
     if verbose:
         print("built", LIB)
     return LIB

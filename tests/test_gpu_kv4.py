@@ -336,6 +336,40 @@ def test_batch_does_not_change_a_sequence():
         assert np.array_equal(_attend(q[b:b + 1], cache[b * each:(b + 1) * each], 128, Hkv, [n], n)[0], whole[b])
 
 
+def test_tensors_that_do_not_fit():
+    """Wrong types, shapes, sizes, devices and strides raise before any launch,
+    and a scratch that is too small is VLA_ERR_SHAPE."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    B, L, H, Hkv, dh, cap = 2, 40, 4, 2, 64, 2048
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    k, q, cache, lens = bf(B, L, Hkv, dh), bf(B, 1, H, dh), _cache(B, Hkv, cap, dh), _i32(40, 40)
+    scratch = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    tab = torch.zeros((4, dh // 2), device="cuda")
+    store = lambda **c: vb.vla_op_kv4_store(**{**dict(k=k, v=k, start=None, count=lens, cache=cache, L_cap=cap), **c})  # noqa: E731
+    attend = lambda **c: vb.vla_op_attention_kv4(**{**dict(q=q, cache=cache, L_cap=cap, Hkv=Hkv, lens=lens, o=q.clone(), max_len=cap, scratch=scratch), **c})  # noqa: E731
+    rope = lambda **c: vb.vla_op_qk_norm_rope(**{**dict(q=q, k=bf(B, 1, Hkv, dh), gq=None, gk=None, eps=0.0, cos=tab, sin=tab, pos=None, q_out=q, k_out=bf(B, 1, Hkv, dh)), **c})  # noqa: E731
+    store(), attend(), rope()
+    for bad in (lambda: store(v=k.float()), lambda: store(v=k[:, :39]), lambda: store(k=k.transpose(2, 3)), lambda: store(count=lens.long()),
+                lambda: store(count=lens[:1]), lambda: store(cache=cache[:-1]), lambda: store(cache=cache.cpu()), lambda: store(L_cap=cap + 32),
+                lambda: store(k=k[0]), lambda: store(start=_i32(0, 0, 0, 0)[::2]), lambda: attend(lens=None), lambda: attend(lens=lens.float()),
+                lambda: attend(o=q.float()), lambda: attend(o=bf(B, 1, H, dh + 64)[..., ::2][..., :dh]), lambda: attend(q=q.cpu()),
+                lambda: attend(Hkv=4), lambda: attend(max_len=1 << 40), lambda: rope(sin=tab[:2]), lambda: rope(gq=tab[0]),
+                lambda: rope(pos=torch.zeros((B, 1), dtype=torch.int64, device="cuda")), lambda: rope(k=k), lambda: rope(q=q.half())):
+        with pytest.raises(ValueError):
+            bad()
+    need = vb.vla_op_attention_kv4_scratch(B, 1, H, Hkv, dh, cap)
+    assert need > 0
+    for small in (None, scratch[:need - 4]):
+        with pytest.raises(vb.VlaError) as e:
+            attend(scratch=small)
+        assert e.value.name == "VLA_ERR_SHAPE"
+    with pytest.raises(vb.VlaError) as e:
+        attend(max_len=cap + 1)
+    assert e.value.name == "VLA_ERR_SHAPE"
+    torch.cuda.synchronize()
+
+
 # ------------------------------------------------------------------- together
 
 @pytest.mark.parametrize("H,Hkv,dh,window", [(14, 2, 64, 0), (4, 4, 128, 40)])
