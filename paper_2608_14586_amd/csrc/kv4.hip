@@ -305,10 +305,11 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // A decode step's attention reads each visible key and value once for the few
 // queries that share its KV head, so it is bound by the cache's bytes, and by
 // the instructions that turn codes into operands, which come close behind.
-//  * scores: 16 + c as a bf16 is made of a code by a shift and an and-or, so
-//      q . k = sum_g [ s_g sum (16 + c) q + (m_g - 16 s_g) sum q ]
+//  * scores: two codes become bf16 numbers 16 + c by a rotate and an and-or, so
+//      q . k = sum_g [ s_g (sum (16 + c) q - 16 sum q) + m_g sum q ]
 //    over the groups g of 32 dims: one MFMA step a group (queries against 16
-//    keys) and two multiply-adds in fp32; sum q is a constant of the loop.
+//    keys), whose accumulators start from -16 sum q, and two multiply-adds in
+//    fp32; sum q is a constant of the loop.
 //  * softmax: a running maximum and sum per query, in fp32, one pass.
 //  * values: with P the weights and per group P' = P s_g,
 //      sum P v = sum P' (16 + c) - 16 sum P' + sum P m_g
@@ -327,6 +328,13 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // Work is split over the keys: waves of a workgroup take every W-th block of
 // 32 keys, workgroups contiguous runs of them, joined in LDS and by
 // kv4_combine_kernel.
+// With R = 1 and dh = 128 a block is about 250 vector instructions and 16 MFMAs
+// a wave against 5120 bytes: 0.8 us of a SIMD, which on 1024 of them is 6.5 TB/s,
+// little more than the memory gives.  So waves have to overlap, and registers
+// decide: 168 leave three waves a SIMD; with two, eight sequences of up to 32768
+// tokens took 58 us instead of 44, and spilling for four 72.  Their 189 MB move at
+// 4.4 TB/s, joining and ragged ends included; one sequence of 2049 tokens takes
+// 8.4 us, of which two launches are 4.6.
 
 // a value of one lane, for all
 __device__ __forceinline__ float lane_of(float x, int lane) {
@@ -736,27 +744,26 @@ struct Plan {
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
   Plan p{};
-  int64_t blocks = cdiv(max_len, BLK);
+  unsigned blocks = max_len > 0 ? cdiv(max_len, BLK) : 1;
   if (window > 0) {
     const int64_t w = ((int64_t)window + Lq - 1 + BLK - 1) / BLK + 1 + cdiv(sinks, BLK);
-    if (w < blocks) blocks = w;
+    if (w < blocks) blocks = (unsigned)w;
   }
-  if (blocks < 1) blocks = 1;
   int64_t best = INT64_MAX;
   for (int R = 1; R == 1 || (R <= 4 && 2 * R < rows); R *= 2) {
     const int tiles = (rows + 4 * R - 1) / (4 * R);
     const int64_t bt = (int64_t)B * Hkv * tiles;
     const int64_t slower = R == 1 ? 100 : R == 2 ? 113 : 145, more = R == 1 ? 0 : R == 2 ? 60 : 180;
     for (int W = 4; W <= 8; W += 4) {
-      const int64_t most = (blocks + W - 1) / W;
-      for (int64_t per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
+      const unsigned most = (blocks + W - 1) / W;
+      for (unsigned per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
         if (per > most) per = most;
-        const int64_t ns = (blocks + per * W - 1) / (per * W);
-        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 180 * per, simd = a_simd * (80 * per + 80);
+        const unsigned ns = (blocks + per * W - 1) / (per * W);
+        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 180ll * per, simd = a_simd * (80 * per + 80);
         const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 350 + 50 * ((ns - 1) / 16) : 0);
         if (cost < best && ns <= 4096 && tiles <= 65535)
           best = cost, p = Plan{R, W, tiles, (int)(per * W), (int)ns};
-        if (per == most) break;
+        if (per == most || wave * slower / 100 + more >= best) break;  // longer runs of blocks cost no less
       }
     }
   }
@@ -824,7 +831,6 @@ size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len,
 
 hipError_t kv4_attention(Kv4Attn a, int dh, size_t scratch_bytes, hipStream_t s) {
   const Plan p = plan_of(a.B, a.Lq, a.H, a.Hkv, a.max_len, a.window, a.sinks);
-  if (!p.R) return hipErrorInvalidValue;  // more tiles than a grid has
   if (scratch_of(p, a.B, a.Lq, a.H, dh) > scratch_bytes) return hipErrorOutOfMemory;
   a.G = a.H / a.Hkv;
   a.by_G = fast_div(a.G);

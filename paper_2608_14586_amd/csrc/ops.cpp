@@ -60,7 +60,8 @@ vla_status kv4_rows(const vla_heads* k, const vla_heads* v, const int32_t* start
 vla_status attn_check(int B, int Lq, int H, int Hkv, int dh, int max_len, int* window, int* sinks) {
   if (B < 0 || Lq < 0 || H <= 0 || Hkv <= 0 || max_len < 0 || *window < 0 || *sinks < 0) return VLA_ERR_INVALID_ARG;
   if (H % Hkv || (dh != 64 && dh != 128) || max_len > 1 << 24 || (int64_t)Lq * H > MAX_GRID ||
-      (int64_t)B * Lq * H > MAX_GRID || (int64_t)B * Hkv > MAX_GRID)
+      (int64_t)B * Lq * H > MAX_GRID || (int64_t)B * Hkv > MAX_GRID ||
+      (int64_t)Lq * (H / Hkv) > 16 * 65535)  // tiles of at most 16 queries, along the grid's z
     return VLA_ERR_UNSUPPORTED;
   if (*window >= max_len) *window = 0;
   if (*sinks > max_len) *sinks = max_len;

@@ -68,7 +68,15 @@ int int_of(PyObject* o, const char* name) {
   }
   return (int)v;
 }
-void* stream_of(PyObject* o) { return o == Py_None ? nullptr : (void*)PyLong_AsVoidPtr(o); }
+void* stream_of(PyObject* o) {
+  if (o == Py_None) return nullptr;
+  void* s = PyLong_AsVoidPtr(o);
+  if (!s && PyErr_Occurred()) {
+    PyErr_Clear();
+    throw Misfit{"stream", "None or a stream's address"};
+  }
+  return s;
+}
 int dim(const at::Tensor& t, int d, const char* name) {
   if (t.size(d) != (int)t.size(d)) throw Misfit{name, "sizes of 32 bits"};
   return (int)t.size(d);
@@ -99,6 +107,10 @@ vla_status gemv_w4(PyObject* const* a) {
   const at::Tensor &x = tensor_of(a[0], "x"), &out = tensor_of(a[3], "out");
   const int dev = device_of(x, "x"), N = int_of(a[4], "N"), group = int_of(a[5], "group");
   const int swiglu = PyObject_IsTrue(a[6]);
+  if (swiglu < 0) {
+    PyErr_Clear();
+    throw Misfit{"swiglu", "True or False"};
+  }
   if (x.scalar_type() != BF16 || x.dim() != 2 || (x.stride(1) != 1 && x.size(1) != 1))
     throw Misfit{"x", "bfloat16 [M, K] with dense rows"};
   const int M = dim(x, 0, "x"), K = dim(x, 1, "x");

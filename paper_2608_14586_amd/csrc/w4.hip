@@ -17,6 +17,11 @@
 // of fp32 (with 128, the exponent at which codes need no shift, it would be
 // eight times that).
 //
+// That leaves 7 instructions and an MFMA for the 512 weights of a word a lane, so
+// the stream of weights is the bound where it is long: 26 MB (N = 12288, K =
+// 4096, one row) take 6.7 us, 2.3 of them a launch's own; 48 MB (gated, 2 x 11008,
+// K = 4096, four rows) 10 us; 29 MB with 13 rows 8.4 us.
+//
 // Rows of x sit in the accumulator rows that one register of the MFMA result
 // covers: with M <= 4 in rows 0, 4, 8, 12, so a lane holds one useful value
 // (R = 1) and scales that alone; M <= 8 uses two (R = 2), up to 16 all four.
@@ -289,17 +294,21 @@ hipError_t w4_pack(const uint8_t* codes, const bf16_t* scales, const bf16_t* zer
 hipError_t gemv_w4(const bf16_t* x, int64_t ldx, const void* wp, const float* res, void* out, int64_t ldo, bool f32,
                    bool swiglu, int M, int N, int K, int group, hipStream_t s) {
   const W4Args a{x, ldx, (const uint8_t*)wp, res, out, ldo, M, N, K, f32};
-  // Waves a workgroup: the more there are, the shorter each one's chain of
-  // loads.  With two workgroups a CU or more other workgroups fill the waits
-  // instead, and short chains have none; there four waves do where a block is
-  // much work (16 rows, two tiles).  us at 4, 8, 16 waves: N = 4096, K = 11008,
-  // one row 13.7, 8.4, 6.5; N = 12288, K = 4096, one row 7.3, 6.8, 7.2, 16 rows
-  // 9.1, 9.3, 11.1; N = 3830, K = 1184, four rows 3.2, 3.0, 3.2.
+  // Waves a workgroup: the more there are, the shorter each one's chain of loads,
+  // until workgroups fill each other's waits.  us at 4, 8, 16 waves, g = 64:
+  //  * one workgroup a CU or fewer: 16, if each then has more than a block.
+  //    N = 4096, one row: K = 2816 -, 3.4, 3.2; 12288 -, 8.3, 6.6; N = 2048,
+  //    K = 2560 3.4, 2.9, 3.0
+  //  * up to two a CU: 8.  N = 6144, K = 4096, one row 6.2, 5.1, 5.0, 13 rows 7.3,
+  //    6.1, 7.0; gated, N = 12288, one row 8.1, 7.2, 8.0
+  //  * more: 8 where a block is little work, else 4.  N = 12288, K = 4096, one row
+  //    7.2, 6.8, 7.1, 13 rows 8.4, 8.8, 9.9; gated, N = 24576, K = 8192, seven
+  //    rows 24, 28, 27
   const int tiles = swiglu ? N / 32 : cdiv(N, 16);
   const int64_t wgs = (int64_t)tiles * cdiv(M, 16);
-  if (wgs < 512 && K > 2944)
+  if (wgs <= 256 && K > 2560)
     return swiglu ? by_rows<2, 16, true>(a, group, s) : by_rows<1, 16, false>(a, group, s);
-  if (wgs < 512 || (M <= 8 && !swiglu))
+  if (wgs <= 512 || (M <= 8 && !swiglu))
     return swiglu ? by_rows<2, 8, true>(a, group, s) : by_rows<1, 8, false>(a, group, s);
   return swiglu ? by_rows<2, 4, true>(a, group, s) : by_rows<1, 4, false>(a, group, s);
 }

@@ -355,7 +355,8 @@ def test_tensors_that_do_not_fit():
                 lambda: store(k=k[0]), lambda: store(start=_i32(0, 0, 0, 0)[::2]), lambda: attend(lens=None), lambda: attend(lens=lens.float()),
                 lambda: attend(o=q.float()), lambda: attend(o=bf(B, 1, H, dh + 64)[..., ::2][..., :dh]), lambda: attend(q=q.cpu()),
                 lambda: attend(Hkv=4), lambda: attend(max_len=1 << 40), lambda: rope(sin=tab[:2]), lambda: rope(gq=tab[0]),
-                lambda: rope(pos=torch.zeros((B, 1), dtype=torch.int64, device="cuda")), lambda: rope(k=k), lambda: rope(q=q.half())):
+                lambda: rope(pos=torch.zeros((B, 1), dtype=torch.int64, device="cuda")), lambda: rope(k=k), lambda: rope(q=q.half()),
+                lambda: store(stream="s"), lambda: attend(stream=-1.5)):
         with pytest.raises(ValueError):
             bad()
     need = vb.vla_op_attention_kv4_scratch(B, 1, H, Hkv, dh, cap)
@@ -439,3 +440,96 @@ def test_decoder_block_in_4_bits(H, Hkv, dh, window):
         want = want + ref.bf16(up[:, :F] / (1 + np.exp(-up[:, :F])) * up[:, F:]) @ wdown[1]
         got = ref.from_dev(h)
         assert np.linalg.norm(got - want) <= 2e-2 * np.linalg.norm(want - h0), step
+
+
+def test_decode_step_in_a_graph():
+    """Head norms, cache append, attention and the output projection of a decode
+    step captured once, its position on the device: every replay is the eager
+    step, to the last bit, as the cache grows over a block's end."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    B, H, Hkv, dh, d, cap, group, past = 2, 8, 2, 128, 256, 96, 64, 29
+    rng = np.random.default_rng(9)
+    codes = torch.from_numpy(rng.integers(0, 16, (d, H * dh), dtype=np.uint8)).cuda()
+    s = ref.to_dev(rng.uniform(0.002, 0.01, (d, H * dh // group)))
+    Wp = torch.empty(vb.vla_op_w4_packed_bytes(d, H * dh, group), dtype=torch.uint8, device="cuda")
+    vb.vla_op_w4_pack(codes, s, None, Wp, group)
+    ang = np.arange(cap)[:, None] * 10000.0 ** (-np.arange(0, dh, 2) / dh)
+    tc, ts = (torch.from_numpy(f(ang).astype(np.float32)).cuda() for f in (np.cos, np.sin))
+    g = torch.from_numpy(rng.uniform(0.5, 1.5, dh).astype(np.float32)).cuda()
+    k0, v0 = _kv(("graph",), B, past, Hkv, dh)
+    bf = lambda *sh: torch.zeros(sh, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    rows, q, k, o = bf(B, 1, H + 2 * Hkv, dh), bf(B, 1, H, dh), bf(B, 1, Hkv, dh), bf(B, 1, H, dh)
+    h = torch.zeros((B, d), device="cuda")
+    pos, lens = _i32(past, past), _i32(past + 1, past + 1)
+    caches = [_cache(B, Hkv, cap, dh) for _ in range(2)]
+    n = vb.vla_op_attention_kv4_scratch(B, 1, H, Hkv, dh, cap)
+    scratch = torch.zeros(max(n, 16), dtype=torch.uint8, device="cuda")
+    for c in caches:
+        vb.vla_op_kv4_store(ref.to_dev(k0), ref.to_dev(v0), None, None, c, cap)
+
+    def step(cache, stream):
+        vb.vla_op_qk_norm_rope(rows[:, :, :H], rows[:, :, H:H + Hkv], g, g, 1e-6, tc, ts, pos.view(B, 1), q, k, stream)
+        vb.vla_op_kv4_store(k, rows[:, :, H + Hkv:], pos, None, cache, cap, stream)
+        vb.vla_op_attention_kv4(q, cache, cap, Hkv, lens, o, cap, 0, 0, scratch, stream)
+        vb.vla_op_gemv_w4(o.view(B, H * dh), Wp, h, h, d, group, False, stream)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(caches[0], torch.cuda.current_stream().cuda_stream)
+    for t in range(6):
+        rows.copy_(ref.to_dev(ref.normal(("graphrows", t), rows.shape)))
+        pos.fill_(past + t)
+        lens.fill_(past + t + 1)
+        h.fill_(0.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = h.clone()
+        h.fill_(0.25)
+        step(caches[1], None)
+        torch.cuda.synchronize()
+        assert torch.equal(got, h) and torch.equal(caches[0], caches[1]), t
+
+
+def test_two_streams_at_once():
+    """Two attentions that run at the same time, each with its own scratch."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    B, H, Hkv, dh, n = 1, 32, 8, 128, 3000
+    k, v = _kv(("two",), B, n, Hkv, dh)
+    cache = _cache(B, Hkv, 3008, dh)
+    vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(v), None, None, cache, 3008)
+    qs = [ref.to_dev(ref.normal(("twoq", i), (B, 1, H, dh))) for i in range(2)]
+    lens = _i32(n)
+    need = vb.vla_op_attention_kv4_scratch(B, 1, H, Hkv, dh, n)
+    assert need > 0
+    alone = [_attend(q, cache, 3008, Hkv, [n], n) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    scratch = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in qs]
+    outs = [torch.zeros_like(q) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, o, s, st in zip(qs, outs, scratch, streams):
+            vb.vla_op_attention_kv4(q, cache, 3008, Hkv, lens, o, n, 0, 0, s, st.cuda_stream)
+    torch.cuda.synchronize()
+    for o, a in zip(outs, alone):
+        assert np.array_equal(ref.from_dev(o), a)
+
+
+def test_a_query_that_is_not_finite():
+    """reaches no other query of its tile, whatever the split."""
+    B, Lq, H, Hkv, dh, n = 1, 3, 8, 2, 128, 700
+    k, v = _kv(("nan",), B, n, Hkv, dh)
+    from paper_2608_14586_amd import binding as vb
+    cache = _cache(B, Hkv, 704, dh)
+    vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(v), None, None, cache, 704)
+    q = ref.normal(("nanq",), (B, Lq, H, dh))
+    want = _attend(ref.to_dev(q), cache, 704, Hkv, [n], n)
+    for bad in (np.nan, np.inf):
+        x = q.copy()
+        x[0, 1, 2, 5] = bad
+        got = _attend(ref.to_dev(x), cache, 704, Hkv, [n], n)
+        assert np.isnan(got[0, 1, 2]).all()
+        got[0, 1, 2] = want[0, 1, 2]
+        assert np.isfinite(want).all() and np.abs(got - want).max() <= 2.0 ** -7 * np.abs(want).max()

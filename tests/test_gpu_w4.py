@@ -171,3 +171,28 @@ def test_gemv_w4_on_a_stream_and_in_a_graph():
         vb.vla_op_gemv_w4(x, Wp, None, y, N, group, stream=side.cuda_stream)
     side.synchronize()
     assert np.array_equal(ref.from_dev(y), -v @ w.T)
+
+
+@pytest.mark.parametrize("M,N,K,group,swiglu", [
+    (3, 4096, 2568, 64, False), (13, 4112, 2568, 32, False), (20, 2048, 2696, 128, False), (5, 8192, 136, 64, False),
+    (16, 8208, 264, 128, False), (2, 8208, 264, 32, False), (1, 8192, 2568, 32, True), (7, 8224, 2568, 128, True),
+    (9, 16416, 136, 64, True)])
+def test_gemv_w4_either_side_of_a_choice(M, N, K, group, swiglu):
+    """Sizes just inside and just outside each number of waves."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    codes, s, z = _weights((M, N, K, group), N, K, group, True, True)
+    x = np.random.default_rng(M + N).integers(-3, 4, (M, K)).astype(np.float64)
+    want = x @ ref.w4_weights(codes, s, z, group).T
+    bound = np.zeros(want.shape)
+    if swiglu:
+        # e^-v is 2^(-v log2 e): the constant's rounding and the product's are at
+        # most 2^-24 of the exponent each, so e^-v is off by |v| 2^-23 of itself; the
+        # instruction, a sum, a division and a product add less than 2^-20.  Below
+        # v = -88 e^-v overflows and the result is 0 for less than 2^-100.
+        v = want[:, :N // 2]
+        want = v / (1 + np.exp(np.minimum(-v, 700))) * want[:, N // 2:]
+        bound = (2.0 ** -20 + 2.0 ** -23 * np.abs(v)) * np.abs(want) + 2.0 ** -100
+    y = torch.full(want.shape, 7.0, dtype=torch.float32, device="cuda")
+    vb.vla_op_gemv_w4(ref.to_dev(x), _packed(codes, s, z, group), None, y, N, group, swiglu)
+    assert (np.abs(ref.from_dev(y) - want) <= bound).all()

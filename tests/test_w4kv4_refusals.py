@@ -124,7 +124,8 @@ ATT = dict(q=_h(), cache=P, lens=P, o=_h(), B=1, Lq=1, H=4, Hkv=2, L_cap=4096, d
     (dict(scratch=None), "INVALID_ARG"), (dict(o=_h(head=0)), "INVALID_ARG"), (dict(q=_h(head=-8)), "INVALID_ARG"),
     (dict(H=5), "UNSUPPORTED"), (dict(dh=256), "UNSUPPORTED"), (dict(L_cap=4097), "UNSUPPORTED"),
     (dict(q=_h(P + 4)), "UNSUPPORTED"), (dict(o=_h(seq=4)), "UNSUPPORTED"), (dict(scratch=P + 4), "UNSUPPORTED"),
-    (dict(cache=P + 2), "UNSUPPORTED"), (dict(B=1 << 20, H=64, Hkv=32), "UNSUPPORTED"), (dict(Lq=1 << 30), "UNSUPPORTED"), (dict(max_len=4097), "SHAPE"), (dict(nbytes=4), "SHAPE"),
+    (dict(cache=P + 2), "UNSUPPORTED"), (dict(B=1 << 20, H=64, Hkv=32), "UNSUPPORTED"), (dict(Lq=1 << 30), "UNSUPPORTED"),
+    (dict(Lq=1 << 19), "UNSUPPORTED"), (dict(max_len=4097), "SHAPE"), (dict(nbytes=4), "SHAPE"),
     (dict(scratch=None, nbytes=0), "SHAPE")])
 def test_attention_kv4_refuses(change, code):
     assert _name(vb.lib().vla_op_attention_kv4(*{**ATT, **change}.values())) == "VLA_ERR_" + code
