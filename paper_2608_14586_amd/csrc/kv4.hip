@@ -329,12 +329,19 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // 32 keys, workgroups contiguous runs of them, joined in LDS and by
 // kv4_combine_kernel.
 // With R = 1 and dh = 128 a block is about 250 vector instructions and 16 MFMAs
-// a wave against 5120 bytes: 0.8 us of a SIMD, which on 1024 of them is 6.5 TB/s,
-// little more than the memory gives.  So waves have to overlap, and registers
-// decide: 168 leave three waves a SIMD; with two, eight sequences of up to 32768
-// tokens took 58 us instead of 44, and spilling for four 72.  Their 189 MB move at
-// 4.4 TB/s, joining and ragged ends included; one sequence of 2049 tokens takes
-// 8.4 us, of which two launches are 4.6.
+// a wave against 5120 bytes.  A wave alone on its SIMD takes 0.8 us a block that
+// lies in cache and 1.2 from memory, two side by side 1.1 and 1.9: the memory
+// comes first.  156 registers leave three waves a SIMD; two took a third longer
+// over long caches, and four spill.  Eight sequences of up to 32768 tokens (32
+// heads, 8 KV heads, 189 MB) take 42.7 us, 4.4 TB/s, joining and ragged ends
+// included; one of 2049 tokens (32 KV heads) 7.9 us, of which two launches are
+// 4.6.
+// The loads of the next block go out in two parts, each into the registers that
+// the part of this block before it has used up, unconditionally and below a
+// scheduling barrier: with branches around them, or with a use of the old values
+// left below them, the compiler waits for every load at the loop's end, which
+// cost 2% of a long cache's time and 10% of short ones'.  A second block ahead
+// gains nothing there and costs a wave a SIMD (43 -> 55 us).
 
 // a value of one lane, for all
 __device__ __forceinline__ float lane_of(float x, int lane) {
@@ -443,8 +450,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   }
   // the blocks of this sequence and head (at most 2^24 tokens: below 2^32 bytes)
   const uint32_t bytes = (uint32_t)(a.L_cap / BLK) * (40 * DH);
-  const __amdgpu_buffer_rsrc_t cache =
-      __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.cache + (size_t)bh * bytes), (short)0, (int)bytes, 0x00020000);
+  const uint8_t* const own = (const uint8_t*)a.cache + (size_t)bh * bytes;
   uint32_t* pw = lds[wave];
   const int prow = (c16 >> 2) * R + min(c16 & 3, R - 1);
   const Unpack uk = Unpack::make<false>(), uv = Unpack::make<true>();
@@ -452,8 +458,14 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   Words<NG> kc[2], kp[2], vp[2];
   Words<ND> vc;
   auto block_of = [&](int j) { return j < sn.sinkb ? j : sn.blk0 + j - sn.sinkb; };
+  // past the run's last block the buffer is empty and the loads touch no memory:
+  // a branch around them would make every wait one for all loads
+  auto buffer = [&](int j) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)own, (short)0, j < j1 ? (int)bytes : 0, 0x00020000);
+  };
   auto fetch_keys = [&](int j) {
     const uint32_t base = (uint32_t)block_of(j) * (40 * DH);
+    const __amdgpu_buffer_rsrc_t cache = buffer(j);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       kc[t] = load_words<NG>(cache, t * 8 * DH + c16 * (DH / 2) + kq * (DH / 8), base);
@@ -462,15 +474,14 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   };
   auto fetch_values = [&](int j) {
     const uint32_t base = (uint32_t)block_of(j) * (40 * DH);
+    const __amdgpu_buffer_rsrc_t cache = buffer(j);
 #pragma unroll
     for (int t = 0; t < 2; ++t) vp[t] = load_words<NG>(cache, 36 * DH + (t * 16 + c16) * NG * 4, base);
     vc = load_words<ND>(cache, 16 * DH + lane * ND * 4, base);
   };
   // the next block's keys and values are on their way as soon as this block's are used up
-  if (j0 + wave < j1) {
-    fetch_keys(j0 + wave);
-    fetch_values(j0 + wave);
-  }
+  fetch_keys(j0 + wave);
+  fetch_values(j0 + wave);
   __builtin_amdgcn_sched_barrier(0);
 
   bf16x8 qa[NG];
@@ -524,7 +535,11 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
 #pragma unroll
         for (int r = 0; r < R; ++r) p[t][r] = fmaf(lo16(kp[t].w[g]), d[g][r], p[t][r]);
     }
-    if (j + W < j1) fetch_keys(j + W);
+    // no use of this block's registers may sink below the loads into them
+#pragma unroll
+    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(p[0][r]), "+v"(p[1][r]));
+    __builtin_amdgcn_sched_barrier(0);
+    fetch_keys(j + W);
     if (!whole) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -622,7 +637,8 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
 #pragma unroll
       for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] = mfma(ph, __builtin_bit_cast(f16x8, uv(vc.w[d])), o[d]);
     }
-    if (j + W < j1) fetch_values(j + W);
+    __builtin_amdgcn_sched_barrier(0);
+    fetch_values(j + W);
   }
 
   // join the waves: lane (c16, kq) holds dims 16 d + c16 of tile rows kq R + r
@@ -730,17 +746,16 @@ struct Plan {
 };
 // Queries a tile (4 R), waves a workgroup and blocks a wave, by the estimated
 // time of each choice, in hundredths of a microsecond: a wave alone on its SIMD
-// takes 180 a block, a SIMD 80 a block and 80 more a wave, 13% and 45% more
-// with R = 2 and 4 (memory latency and the LDS round trip weigh more than
-// instructions; dh hardly shows), and a launch 60 and 180 more; one CU takes
-// the workgroups past 256; joining splits costs 350, and 50 more past every 16
-// splits.  Over 46 calls timed at every choice of the last two (1 to 64
-// sequences, 1 to 131072 tokens, R = 1, 2, 4, windows), up to 34 each, what
-// this takes is 0.2% slower than the fastest on average and 3% at most; a fixed
-// aim of 1024 workgroups of four waves lost up to 40%.  Smaller tiles than the
-// queries need unpack the cache again for each, but where whole ones leave CUs
-// idle they are faster: 16 sequences of 12 queries over 8 heads and a window of
-// 1024, one tile 14.3 us, two 11.0.
+// takes 80 a block, a SIMD 37 a block and 32 more a wave, 13% and 50% more with
+// R = 2 and 4 (instruction latency and the LDS round trip weigh more than
+// instructions; dh hardly shows), and a launch 46 more; one CU takes the
+// workgroups past 256; joining splits costs 360, and 44 more past every 16
+// splits.  Over 80 calls timed at every choice (1 to 128 sequences, 1 to 131072
+// tokens, 1 to 256 queries a KV head, windows), up to 64 each, what this takes is
+// 0.4% slower than the fastest on average and 5% at most.  Smaller tiles than
+// the queries need unpack the cache again for each, but where whole ones leave
+// CUs idle they are faster: 16 sequences of 12 queries over 8 heads and a window
+// of 1024, one tile 13.5 us, two 10.2.
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
   Plan p{};
@@ -753,14 +768,14 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
   for (int R = 1; R == 1 || (R <= 4 && 2 * R < rows); R *= 2) {
     const int tiles = (rows + 4 * R - 1) / (4 * R);
     const int64_t bt = (int64_t)B * Hkv * tiles;
-    const int64_t slower = R == 1 ? 100 : R == 2 ? 113 : 145, more = R == 1 ? 0 : R == 2 ? 60 : 180;
+    const int64_t slower = R == 1 ? 100 : R == 2 ? 113 : 150, more = R == 1 ? 0 : 46;
     for (int W = 4; W <= 8; W += 4) {
       const unsigned most = (blocks + W - 1) / W;
       for (unsigned per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
         if (per > most) per = most;
         const unsigned ns = (blocks + per * W - 1) / (per * W);
-        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 180ll * per, simd = a_simd * (80 * per + 80);
-        const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 350 + 50 * ((ns - 1) / 16) : 0);
+        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 80ll * per, simd = a_simd * (37 * per + 32);
+        const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 360 + 44 * ((ns - 1) / 16) : 0);
         if (cost < best && ns <= 4096 && tiles <= 65535)
           best = cost, p = Plan{R, W, tiles, (int)(per * W), (int)ns};
         if (per == most || wave * slower / 100 + more >= best) break;  // longer runs of blocks cost no less
