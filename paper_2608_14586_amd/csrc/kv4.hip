@@ -464,7 +464,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     return __builtin_amdgcn_make_buffer_rsrc((void*)own, (short)0, j < j1 ? (int)bytes : 0, 0x00020000);
   };
   auto fetch_keys = [&](int j) {
-    const uint32_t base = (uint32_t)block_of(j) * (40 * DH);
+    const uint32_t base = j < j1 ? (uint32_t)block_of(j) * (40 * DH) : 0;
     const __amdgpu_buffer_rsrc_t cache = buffer(j);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -473,7 +473,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     }
   };
   auto fetch_values = [&](int j) {
-    const uint32_t base = (uint32_t)block_of(j) * (40 * DH);
+    const uint32_t base = j < j1 ? (uint32_t)block_of(j) * (40 * DH) : 0;
     const __amdgpu_buffer_rsrc_t cache = buffer(j);
 #pragma unroll
     for (int t = 0; t < 2; ++t) vp[t] = load_words<NG>(cache, 36 * DH + (t * 16 + c16) * NG * 4, base);

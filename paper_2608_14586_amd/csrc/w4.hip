@@ -19,8 +19,8 @@
 //
 // That leaves 7 instructions and an MFMA for the 512 weights of a word a lane, so
 // the stream of weights is the bound where it is long: 26 MB (N = 12288, K =
-// 4096, one row) take 6.7 us, 2.3 of them a launch's own; 48 MB (gated, 2 x 11008,
-// K = 4096, four rows) 10 us; 29 MB with 13 rows 8.4 us.
+// 4096, one row) take 6.5 us, 2.3 of them a launch's own; 48 MB (gated, 2 x 11008,
+// K = 4096, four rows) 10 us; 29 MB with 13 rows (N = 4096, K = 11008) 8.6 us.
 //
 // Rows of x sit in the accumulator rows that one register of the MFMA result
 // covers: with M <= 4 in rows 0, 4, 8, 12, so a lane holds one useful value
@@ -93,13 +93,13 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
   const int t0 = blockIdx.x * TW;
   const int m0 = blockIdx.y * 16;
   const uint8_t* codes[NT];
-  const uint32_t* params[NT];
+  const uint8_t* params[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int t = SWIGLU ? (i < TW ? min(t0 + i, ntiles / 2 - 1) : ntiles / 2 + min(t0 + i - TW, ntiles / 2 - 1))
                          : min(t0 + i, ntiles - 1);
     codes[i] = a.wp + (size_t)t * KB * 1024;
-    params[i] = (const uint32_t*)(a.wp + code_bytes(a.N, a.K)) + (size_t)t * KB * 16 * GPB;
+    params[i] = a.wp + code_bytes(a.N, a.K) + (size_t)t * KB * (64 * GPB);
   }
   const int mrows = min(a.M - m0, 16);
   const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(
@@ -118,10 +118,6 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
   // outside the buffer and read as zero.  LDS turns them into operands: MFMA row
   // 4 i + r is row i R + r (r < R; the others repeat one, their results are not
   // used); word c of row m lies at c ^ 4 (m & 3), free of bank conflicts.
-  // whether the next block's x is asked for before the products or after them:
-  // before, except at 16 rows, whose 16 registers are better asked for last (9.5 -> 8.8 us
-  // at 13 rows, N = 4096, K = 11008; 7.2 -> 6.5 the other way at one row)
-  constexpr bool EARLY_X = R != 4;
   u32x4* xs = lds[wave];
   uint32_t xat[R];
 #pragma unroll
@@ -132,31 +128,59 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
   const int xput = kq * 16 + (c16 ^ kq * 4);
   const int xrow = (c16 >> 2) * R + min(c16 & 3, R - 1), xget = xrow * 16, xswz = (xrow & 3) * 4;
 
-  u32x4 cw[NT], xw[R];
+  // a block's registers, loaded again as soon as they are used up, in parts.  Past
+  // the last block the buffers are empty and the loads touch no memory: with a
+  // branch around them, with uses of the old values below them or with the first
+  // loads in another order than the loop's, the compiler waits for every load at
+  // the loop's end (2 to 8% of the time).  A second block ahead costs waves: 6.5 ->
+  // 7.0 us at N = 12288, K = 4096, one row.
+  u32x4 xw[R], cw[NT];
   Params<GPB> pw[NT];
-  auto load_x = [&](int kb) {
+  // x of 16 rows is 16 registers, and asked for after the codes (N = 4096, K = 11008,
+  // 13 rows: 8.6 us, before them 9.2)
+  constexpr bool LATE_X = R == 4;
+  auto fetch_x = [&](int kb) {
     const bool in = kb * 128 + c16 * 8 < a.K;
 #pragma unroll
     for (int q = 0; q < R; ++q)
       xw[q] = __builtin_bit_cast(
           u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, in ? xat[q] + kb * 256 : 0x80000000u, 0, 0));
   };
-  auto load_w = [&](int kb) {
+  auto fetch_codes = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      cw[i] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     __builtin_amdgcn_make_buffer_rsrc((void*)codes[i], (short)0, kb < KB ? KB * 1024 : 0, 0x00020000),
+                     lane * 16, kb < KB ? kb * 1024 : 0, 0));
+  };
+  auto fetch_params = [&](int kb) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      cw[i] = *(const u32x4*)(codes[i] + (size_t)kb * 1024 + lane * 16);
-      pw[i] = ((const Params<GPB>*)params[i])[kb * 16 + c16];
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)params[i], (short)0, kb < KB ? KB * (64 * GPB) : 0, 0x00020000);
+      const uint32_t at = c16 * (4 * GPB), base = kb < KB ? kb * (64 * GPB) : 0;
+      if constexpr (GPB == 1)
+        pw[i].w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, at, base, 0);
+      else if constexpr (GPB == 2)
+        pw[i] = __builtin_bit_cast(Params<2>, __builtin_amdgcn_raw_buffer_load_b64(r, at, base, 0));
+      else
+        pw[i] = __builtin_bit_cast(Params<4>, __builtin_amdgcn_raw_buffer_load_b128(r, at, base, 0));
     }
   };
-  // a block's registers are loaded again as soon as they are used up
-  if (wave < KB) {
-    load_w(wave);
-    load_x(wave);
-  }
+  if (!LATE_X) fetch_x(wave);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_codes(wave);
+  __builtin_amdgcn_sched_barrier(0);
+  if (LATE_X) fetch_x(wave);
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_params(wave);
+  __builtin_amdgcn_sched_barrier(0);
   for (int kb = wave; kb < KB; kb += W) {
-    const bool more = kb + W < KB;
 #pragma unroll
     for (int q = 0; q < R; ++q) xs[q * 64 + xput] = xw[q];
+    __builtin_amdgcn_sched_barrier(0);
+    if (!LATE_X) fetch_x(kb + W);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     bf16x8 xa[4];
@@ -164,7 +188,6 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
     for (int t = 0; t < 4; ++t) xa[t] = __builtin_bit_cast(bf16x8, xs[xget + ((t * 4 + kq) ^ xswz)]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    if (EARLY_X && more) load_x(kb + W);
     f32x4 sum[GPB], d[GPB][NT];
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
@@ -185,20 +208,21 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
 #pragma unroll
       for (int i = 0; i < NT; ++i) asm volatile("" : "+v"(d[g][i]));
     }
-    Params<GPB> pv[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) pv[i] = pw[i];
-    if (more) load_w(kb + W);
-    if (!EARLY_X && more) load_x(kb + W);
+    __builtin_amdgcn_sched_barrier(0);
+    fetch_codes(kb + W);
+    __builtin_amdgcn_sched_barrier(0);
+    if (LATE_X) fetch_x(kb + W);
 #pragma unroll
     for (int g = 0; g < GPB; ++g)
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const uint32_t p = pv[i].w[g];
+        const uint32_t p = pw[i].w[g];
         const float s = __uint_as_float(p << 16), z = __uint_as_float(p & 0xffff0000u);
 #pragma unroll
         for (int r = 0; r < R; ++r) y[i][r] = fmaf(s, fmaf(-16.f - z, sum[g][r], d[g][i][r]), y[i][r]);
       }
+    __builtin_amdgcn_sched_barrier(0);
+    fetch_params(kb + W);
   }
   float* red = (float*)lds[wave];
 #pragma unroll
@@ -294,21 +318,21 @@ hipError_t w4_pack(const uint8_t* codes, const bf16_t* scales, const bf16_t* zer
 hipError_t gemv_w4(const bf16_t* x, int64_t ldx, const void* wp, const float* res, void* out, int64_t ldo, bool f32,
                    bool swiglu, int M, int N, int K, int group, hipStream_t s) {
   const W4Args a{x, ldx, (const uint8_t*)wp, res, out, ldo, M, N, K, f32};
-  // Waves a workgroup: the more there are, the shorter each one's chain of loads,
+  // Waves a workgroup: the more there are, the shorter each one's chain of blocks,
   // until workgroups fill each other's waits.  us at 4, 8, 16 waves, g = 64:
-  //  * one workgroup a CU or fewer: 16, if each then has more than a block.
-  //    N = 4096, one row: K = 2816 -, 3.4, 3.2; 12288 -, 8.3, 6.6; N = 2048,
-  //    K = 2560 3.4, 2.9, 3.0
-  //  * up to two a CU: 8.  N = 6144, K = 4096, one row 6.2, 5.1, 5.0, 13 rows 7.3,
-  //    6.1, 7.0; gated, N = 12288, one row 8.1, 7.2, 8.0
-  //  * more: 8 where a block is little work, else 4.  N = 12288, K = 4096, one row
-  //    7.2, 6.8, 7.1, 13 rows 8.4, 8.8, 9.9; gated, N = 24576, K = 8192, seven
-  //    rows 24, 28, 27
+  //  * one workgroup a CU or fewer: 16 if 8 would have more than four blocks each,
+  //    else 8.  N = 4096, K = 12288, one row 11.7, 7.8, 6.4, 13 rows 15.1, 9.5, 8.5;
+  //    N = 2048, K = 4096, 3.8, 3.1, 3.2 and 4.8, 4.1, 4.2
+  //  * up to two a CU: 8, or 4 if 8 would have one block each.  N = 6144, K = 4096,
+  //    one row 5.9, 4.8, 4.9, 13 rows 7.0, 6.2, 7.0; gated, N = 12288, K = 896, one
+  //    row 3.0, 3.1, 3.6
+  //  * more: the same where a block is little work, else 4.  N = 12288, K = 4096,
+  //    one row 6.6, 6.4, 6.8, 13 rows 8.1, 8.7, 9.1; N = 8448, K = 896, one row 2.8,
+  //    2.9, 3.3; gated, N = 24576, K = 4096, 13 rows 11.5, 12.3, 15.0
   const int tiles = swiglu ? N / 32 : cdiv(N, 16);
   const int64_t wgs = (int64_t)tiles * cdiv(M, 16);
-  if (wgs <= 256 && K > 2560)
-    return swiglu ? by_rows<2, 16, true>(a, group, s) : by_rows<1, 16, false>(a, group, s);
-  if (wgs <= 512 || (M <= 8 && !swiglu))
+  if (wgs <= 256 && K > 4096) return swiglu ? by_rows<2, 16, true>(a, group, s) : by_rows<1, 16, false>(a, group, s);
+  if ((wgs <= 256 || K > 1024) && (wgs <= 512 || (M <= 4 && !swiglu)))
     return swiglu ? by_rows<2, 8, true>(a, group, s) : by_rows<1, 8, false>(a, group, s);
   return swiglu ? by_rows<2, 4, true>(a, group, s) : by_rows<1, 4, false>(a, group, s);
 }

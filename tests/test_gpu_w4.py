@@ -174,7 +174,8 @@ def test_gemv_w4_on_a_stream_and_in_a_graph():
 
 
 @pytest.mark.parametrize("M,N,K,group,swiglu", [
-    (3, 4096, 2568, 64, False), (13, 4112, 2568, 32, False), (20, 2048, 2696, 128, False), (5, 8192, 136, 64, False),
+    (3, 4096, 2568, 64, False), (13, 4112, 2568, 32, False), (1, 4096, 4104, 32, False), (12, 4112, 4104, 64, False),
+    (5, 4112, 1032, 128, False), (6, 8224, 1024, 64, True), (20, 2048, 2696, 128, False), (5, 8192, 136, 64, False),
     (16, 8208, 264, 128, False), (2, 8208, 264, 32, False), (1, 8192, 2568, 32, True), (7, 8224, 2568, 128, True),
     (9, 16416, 136, 64, True)])
 def test_gemv_w4_either_side_of_a_choice(M, N, K, group, swiglu):
