@@ -264,11 +264,46 @@ hipError_t launch(const W4Args& a, int group, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int NT, int W, bool SWIGLU>
-hipError_t by_rows(const W4Args& a, int group, hipStream_t s) {
-  if (a.M <= 4) return launch<NT, 1, W, SWIGLU>(a, group, s);
-  if (a.M <= 8) return launch<NT, 2, W, SWIGLU>(a, group, s);
-  return launch<NT, 4, W, SWIGLU>(a, group, s);
+template <int NT, int W>
+hipError_t by_rows(const W4Args& a, int group, bool swiglu, hipStream_t s) {
+  if constexpr (NT > 1) {
+    if (swiglu)
+      return a.M <= 4   ? launch<NT, 1, W, true>(a, group, s)
+             : a.M <= 8 ? launch<NT, 2, W, true>(a, group, s)
+                        : launch<NT, 4, W, true>(a, group, s);
+  }
+  return a.M <= 4   ? launch<NT, 1, W, false>(a, group, s)
+         : a.M <= 8 ? launch<NT, 2, W, false>(a, group, s)
+                    : launch<NT, 4, W, false>(a, group, s);
+}
+
+// Tiles and waves a workgroup, by the estimated time of each choice, in
+// hundredths of a microsecond: a wave takes 70 a block of 128 k and 7 more a tile,
+// a SIMD 12 a tile and block, 9 a block for x past four rows and 18 a wave; one CU
+// takes the workgroups past 256; a tile costs 37 at the ends.  More waves shorten
+// each one's chain of blocks, more tiles share the turning of x into operands, and
+// both leave fewer workgroups.  Over 332 calls timed at every choice (N = 1024 to
+// 57344, K = 896 to 16384, 1 to 13 rows, plain and gated) what this takes is 0.6%
+// slower than the fastest on average and 9% at most, and over 110 others, drawn
+// from N = 32 to 160000 and K = 64 to 32768, 0.5% and 7%.  us, tiles x waves:
+//   N = 4096, K = 16384, 13 rows, g = 128:  1 x 8 10.4, 1 x 16 9.6
+//   N = 8192, K = 8192, 13 rows, g = 32:  1 x 8 11.0, 2 x 16 9.9
+//   N = 28672, K = 8192, 13 rows, g = 128:  1 x 4 39.6, 4 x 4 26.4
+//   N = 57344, K = 8192, one row:  1 x 8 46.7, 2 x 16 39.7; seven 1 x 4 66, 2 x 8 49
+struct Shape {
+  int tiles, waves;
+};
+Shape shape_of(int M, int N, int K, bool swiglu) {
+  Shape best{};
+  int64_t least = INT64_MAX;
+  for (int n = swiglu ? 2 : 1; n <= 4; n *= 2)
+    for (int w = 4; w <= (n < 4 ? 16 : 8); w *= 2) {
+      const int64_t wgs = (int64_t)cdiv(cdiv(N, 16), n) * cdiv(M, 16), per = cdiv(cdiv(K, 128), w);
+      const int64_t chain = per * (70 + 7 * n), simd = (wgs + 255) / 256 * (w / 4) * (per * ((M > 4 ? 9 : 0) + 12 * n) + 18);
+      const int64_t cost = (chain > simd ? chain : simd) + 37 * n;
+      if (cost < least) least = cost, best = Shape{n, w};
+    }
+  return best;
 }
 
 // one thread per word of the packed weights
@@ -318,23 +353,15 @@ hipError_t w4_pack(const uint8_t* codes, const bf16_t* scales, const bf16_t* zer
 hipError_t gemv_w4(const bf16_t* x, int64_t ldx, const void* wp, const float* res, void* out, int64_t ldo, bool f32,
                    bool swiglu, int M, int N, int K, int group, hipStream_t s) {
   const W4Args a{x, ldx, (const uint8_t*)wp, res, out, ldo, M, N, K, f32};
-  // Waves a workgroup: the more there are, the shorter each one's chain of blocks,
-  // until workgroups fill each other's waits.  us at 4, 8, 16 waves, g = 64:
-  //  * one workgroup a CU or fewer: 16 if 8 would have more than four blocks each,
-  //    else 8.  N = 4096, K = 12288, one row 11.7, 7.8, 6.4, 13 rows 15.1, 9.5, 8.5;
-  //    N = 2048, K = 4096, 3.8, 3.1, 3.2 and 4.8, 4.1, 4.2
-  //  * up to two a CU: 8, or 4 if 8 would have one block each.  N = 6144, K = 4096,
-  //    one row 5.9, 4.8, 4.9, 13 rows 7.0, 6.2, 7.0; gated, N = 12288, K = 896, one
-  //    row 3.0, 3.1, 3.6
-  //  * more: the same where a block is little work, else 4.  N = 12288, K = 4096,
-  //    one row 6.6, 6.4, 6.8, 13 rows 8.1, 8.7, 9.1; N = 8448, K = 896, one row 2.8,
-  //    2.9, 3.3; gated, N = 24576, K = 4096, 13 rows 11.5, 12.3, 15.0
-  const int tiles = swiglu ? N / 32 : cdiv(N, 16);
-  const int64_t wgs = (int64_t)tiles * cdiv(M, 16);
-  if (wgs <= 256 && K > 4096) return swiglu ? by_rows<2, 16, true>(a, group, s) : by_rows<1, 16, false>(a, group, s);
-  if ((wgs <= 256 || K > 1024) && (wgs <= 512 || (M <= 4 && !swiglu)))
-    return swiglu ? by_rows<2, 8, true>(a, group, s) : by_rows<1, 8, false>(a, group, s);
-  return swiglu ? by_rows<2, 4, true>(a, group, s) : by_rows<1, 4, false>(a, group, s);
+  const Shape h = shape_of(M, N, K, swiglu);
+  if (h.tiles == 4) return h.waves == 8 ? by_rows<4, 8>(a, group, swiglu, s) : by_rows<4, 4>(a, group, swiglu, s);
+  if (h.tiles == 2)
+    return h.waves == 16  ? by_rows<2, 16>(a, group, swiglu, s)
+           : h.waves == 8 ? by_rows<2, 8>(a, group, swiglu, s)
+                          : by_rows<2, 4>(a, group, swiglu, s);
+  return h.waves == 16  ? by_rows<1, 16>(a, group, false, s)
+         : h.waves == 8 ? by_rows<1, 8>(a, group, false, s)
+                        : by_rows<1, 4>(a, group, false, s);
 }
 
 }  // namespace vla

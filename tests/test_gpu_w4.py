@@ -177,9 +177,15 @@ def test_gemv_w4_on_a_stream_and_in_a_graph():
     (3, 4096, 2568, 64, False), (13, 4112, 2568, 32, False), (1, 4096, 4104, 32, False), (12, 4112, 4104, 64, False),
     (5, 4112, 1032, 128, False), (6, 8224, 1024, 64, True), (20, 2048, 2696, 128, False), (5, 8192, 136, 64, False),
     (16, 8208, 264, 128, False), (2, 8208, 264, 32, False), (1, 8192, 2568, 32, True), (7, 8224, 2568, 128, True),
-    (9, 16416, 136, 64, True)])
+    (9, 16416, 136, 64, True),
+    (1, 20520, 136, 32, False), (3, 12330, 1544, 64, False), (2, 4130, 3336, 128, False), (6, 12330, 136, 128, False),
+    (7, 4130, 520, 32, False), (5, 4130, 8200, 64, False), (8, 41000, 136, 64, False), (6, 12340, 2568, 128, False),
+    (13, 41000, 136, 32, False), (16, 12340, 2568, 64, False), (30, 12330, 136, 128, False), (1, 152070, 264, 64, False),
+    (6, 41056, 136, 32, True), (8, 8224, 2568, 64, True), (11, 41056, 136, 128, True), (16, 8224, 2568, 32, True),
+    (2, 152096, 136, 32, True)])
 def test_gemv_w4_either_side_of_a_choice(M, N, K, group, swiglu):
-    """Sizes just inside and just outside each number of waves."""
+    """Sizes that take each number of waves and tiles, with ends inside a
+    workgroup's tiles."""
     import torch
     from paper_2608_14586_amd import binding as vb
     codes, s, z = _weights((M, N, K, group), N, K, group, True, True)
