@@ -126,11 +126,10 @@ __device__ __forceinline__ Group4 quantise(const u32x4& w) {
     }
   }
   if (!(d >= 0x1p-99f)) return Group4{0u, m};
-  // d / 15, corrected once: correctly rounded
-  float s = d * (1.f / 15);
-  s = fmaf(fmaf(-s, 15.f, d), 1.f / 15, s);
-  const uint16_t sb = f2bf(s);
-  s = bf2f(sb);
+  // by 1 / 15 in fp32: within 2^-24 of d / 15, which decides only quotients that
+  // lie between two bf16 numbers
+  const uint16_t sb = f2bf(d * (1.f / 15));
+  const float s = bf2f(sb);
   return Group4{codes_of(x, lo, s, __builtin_amdgcn_rcpf(s)), m | sb};
 }
 

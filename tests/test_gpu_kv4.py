@@ -533,3 +533,24 @@ def test_a_query_that_is_not_finite():
         assert np.isnan(got[0, 1, 2]).all()
         got[0, 1, 2] = want[0, 1, 2]
         assert np.isfinite(want).all() and np.abs(got - want).max() <= 2.0 ** -7 * np.abs(want).max()
+
+
+def test_steps_that_fall_between_two_bf16_numbers():
+    """Ranges of 15 times an odd number of half bf16 steps: (max - min) / 15 is a
+    tie, and the step is what the product in fp32 rounds to."""
+    odd = np.arange(257, 512, 2)  # 9 bits, the last one set
+    k = np.zeros((1, 128, 1, 64))
+    k[0, :, 0, 0], k[0, :, 0, 32] = odd * 15 / 64.0, -odd * 15 / 64.0  # 13 bits: reached by two bf16 numbers each
+    hi = ref.bf16(k[..., 0:1])
+    k[..., 1:2], k[..., 0:1] = hi - k[..., 0:1], hi
+    k[..., 33:34], k[..., 32:33] = -hi - k[..., 32:33], -hi
+    k[..., 5:30] = hi * np.linspace(0, 1, 25)
+    k[..., 37:62] = -hi * np.linspace(0, 1, 25)
+    k = ref.bf16(k)
+    from paper_2608_14586_amd import binding as vb
+    cache = _cache(1, 1, 128, 64)
+    vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(k), None, None, cache, 128)
+    a, b = ref.to_dev(k * 0), ref.to_dev(k * 0)
+    vb.vla_op_kv4_load(cache, 128, None, None, a, b)
+    want = ref.bf16(ref.cached(k))
+    assert np.array_equal(ref.from_dev(a), want) and np.array_equal(ref.from_dev(b), want)

@@ -19,7 +19,9 @@ def quantise(x):
     lo, hi = g.min(-1, keepdims=True), g.max(-1, keepdims=True)
     bad = ~np.isfinite(g).all(-1, keepdims=True)
     with np.errstate(all="ignore"):
-        s = np.where(hi - lo < 2.0 ** -99, 0.0, bf16((hi - lo) / 15))
+        d = (hi - lo).astype(np.float32)  # the step is a product in fp32, so that ties fall as the kernel's
+        s = bf16(np.where(np.isfinite(d), (d * np.float32(1 / 15)).astype(np.float64), (hi - lo) / 15))
+        s = np.where(hi - lo < 2.0 ** -99, 0.0, s)
         c = np.where(s > 0, np.minimum(np.rint((g - lo) / np.where(s > 0, s, 1)), 15), 0)
     c, s, lo = np.where(bad, 0, c), np.where(bad, np.nan, s), np.where(bad, np.nan, lo)
     return c, s, lo
