@@ -749,9 +749,9 @@ struct Plan {
 // R = 2 and 4 (instruction latency and the LDS round trip weigh more than
 // instructions; dh hardly shows), and a launch 46 more; one CU takes the
 // workgroups past 256; joining splits costs 360, and 44 more past every 16
-// splits.  Over 80 calls timed at every choice (1 to 128 sequences, 1 to 131072
-// tokens, 1 to 256 queries a KV head, windows), up to 64 each, what this takes is
-// 0.4% slower than the fastest on average and 5% at most.  Smaller tiles than
+// splits.  Over 86 calls timed at every choice (1 to 128 sequences, 1 to 131072
+// tokens, 1 to 256 queries a KV head, windows), up to 100 each, what this takes is
+// 0.5% slower than the fastest on average and 7% at most.  Smaller tiles than
 // the queries need unpack the cache again for each, but where whole ones leave
 // CUs idle they are faster: 16 sequences of 12 queries over 8 heads and a window
 // of 1024, one tile 13.5 us, two 10.2.
@@ -770,15 +770,19 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
     const int64_t slower = R == 1 ? 100 : R == 2 ? 113 : 150, more = R == 1 ? 0 : 46;
     for (int W = 4; W <= 8; W += 4) {
       const unsigned most = (blocks + W - 1) / W;
-      for (unsigned per = 1;; per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4) {
-        if (per > most) per = most;
+      auto consider = [&](unsigned per) {
         const unsigned ns = (blocks + per * W - 1) / (per * W);
         const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 80ll * per, simd = a_simd * (37 * per + 32);
         const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 360 + 44 * ((ns - 1) / 16) : 0);
         if (cost < best && ns <= 4096 && tiles <= 65535)
           best = cost, p = Plan{R, W, tiles, (int)(per * W), (int)ns};
-        if (per == most || wave * slower / 100 + more >= best) break;  // longer runs of blocks cost no less
-      }
+        return wave * slower / 100 + more < best;  // else longer runs of blocks cost no less
+      };
+      // runs that fill all CUs equally, then short ones by ones and longer ones by quarters
+      for (int64_t wgs = 256; wgs <= 1024; wgs += 256)
+        if (wgs >= bt) consider((unsigned)((most + wgs / bt - 1) / (wgs / bt)));
+      for (unsigned per = 1; per < most && consider(per);) per += per < 6 ? 1 : per < 12 ? 2 : per < 24 ? 4 : per / 4;
+      consider(most);
     }
   }
   return p;
