@@ -93,7 +93,8 @@ vla_status vla_op_norm_bf16(const float *x, const float *g, const float *b, floa
  * a graph.  All pointers belong to the current device.  An argument that is
  * missing, negative or not one of its choices is VLA_ERR_INVALID_ARG; a size,
  * stride or alignment that the kernels do not take VLA_ERR_UNSUPPORTED.  Sizes
- * of zero (rows, sequences, tokens) are valid and launch nothing.
+ * of zero (rows, sequences, tokens) are valid and launch nothing.  What a call
+ * writes overlaps nothing else of it, but where its text allows it.
  */
 
 /* Head rows of several sequences: element (b, t, h, d) lies at
