@@ -1,7 +1,7 @@
 // The KV cache in 4 bits: rows into it, rows out of it, and attention over it.
 //
-// Every 32 dims of a key or value row are one group of 16 levels: s =
-// bf16((max - min) / 15), m = min (a bf16 number already), code = (x - m) / s
+// Every 32 dims of a key or value row are one group of 16 levels: s = (max -
+// min) * (1 / 15) in bf16, m = min (a bf16 number already), code = (x - m) / s
 // to the nearest, ties to the even one; the row stands for m + s code.
 //
 // The cache of one sequence and KV head is a run of blocks of 32 tokens, 40 dh
@@ -11,14 +11,18 @@
 //                4 + j / 2 (odd j), the word then rotated left by 3
 //   value codes  [quarter 4][d % 16][d / 16] words: the 8 codes of dim d of
 //                tokens 4 quarter + i (nibble i) and 16 + 4 quarter + i (nibble
-//                4 + i), i < 4, the word then rotated left by 6
+//                4 + i), i < 4, nibbles 3 and 7 exchanged, the word then rotated
+//                left by 6
 //   key params   [token 32][group] words: s in the low half, m in the high
 //   value params [token 32][group] words
 // In this order a wave's loads of keys and values are contiguous and every
-// 32-bit word of codes is one lane's operand of an MFMA step: nibbles i and 4 +
-// i, shifted together to the top mantissa bits of 16.0 in bf16 (keys: bits 3-6)
-// or fp16 (values: bits 6-9), make two operands 16 + c by one shift and one
-// and-or; the rotation saves the first pair its shift.
+// 32-bit word of codes is one lane's operand of an MFMA step, nibbles i and 4 +
+// i two numbers of it.  Keys become bf16: rotated to the top mantissa bits (3-6)
+// of 16.0 they are 16 + c, by one rotate and one and-or a pair; the layout saves
+// the first pair its rotate.  Values become fp16, whose 10 bits of mantissa
+// hold two nibbles: at bits 6-9 of 16.0 one is 16 + c, at bits 2-5 of 256.0 it is
+// 256 + c, so one rotate by 8 serves all four pairs: 5 instructions a word in
+// place of 7, 1 to 3% of attention's time.
 #include "kernels.h"
 
 namespace vla {
@@ -36,20 +40,30 @@ constexpr float UNIT = 64.f;  // what a step is at most as fp16: with RAISE 2^14
 constexpr int KROT = 3, VROT = 6;
 __host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
 
-// Words of codes to operands 16 + c.  The two constants sit in registers of
-// their own, hidden from the compiler: and-or takes no literals, and two
-// instructions in its place cost a third of the loop's unpacking.
-struct Unpack {
-  uint32_t bias, mask;
-  template <bool F16>
-  static __device__ __forceinline__ Unpack make() {
-    Unpack u{F16 ? 0x4c004c00u : 0x41804180u, F16 ? 0x03c003c0u : 0x00780078u};
-    asm("" : "+s"(u.bias), "+v"(u.mask));
-    return u;
+// Words of codes to operands.  The constants sit in registers of their own,
+// hidden from the compiler: and-or takes no literals, and two instructions in its
+// place cost a third of the loop's unpacking.
+struct UnpackKeys {
+  uint32_t bias = 0x41804180u, mask = 0x00780078u;
+  __device__ __forceinline__ UnpackKeys() { asm("" : "+s"(bias), "+v"(mask)); }
+  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
+    const u32x4 v = {(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
+                     (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias,
+                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
+    return __builtin_bit_cast(bf16x8, v);
   }
-  __device__ __forceinline__ u32x4 operator()(uint32_t w) const {
-    return u32x4{(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
-                 (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
+};
+// pairs 0 and 2 are 16 + c, pairs 1 and 3 256 + c
+struct UnpackValues {
+  uint32_t bias16 = 0x4c004c00u, mask16 = 0x03c003c0u, bias256 = 0x5c005c00u, mask256 = 0x003c003cu;
+  __device__ __forceinline__ UnpackValues() {
+    asm("" : "+s"(bias16), "+v"(mask16));
+    asm("" : "+s"(bias256), "+v"(mask256));
+  }
+  __device__ __forceinline__ f16x8 operator()(uint32_t w) const {
+    const uint32_t r = __builtin_amdgcn_alignbit(w, w, 8);
+    const u32x4 v = {(w & mask16) | bias16, (r & mask256) | bias256, (r & mask16) | bias16, (w & mask256) | bias256};
+    return __builtin_bit_cast(f16x8, v);
   }
 };
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
@@ -157,8 +171,10 @@ __device__ __forceinline__ void transpose8(uint32_t (&w)[8]) {
 // dim 8 j + e of a token is code nibble_of(e) of its word j
 __host__ __device__ constexpr int nibble_of(int e) { return e / 2 + (e & 1) * 4; }
 __host__ __device__ constexpr int dim_of(int nibble) { return nibble % 4 * 2 + nibble / 4; }
-// token i of a quarter's eight is token_of(quarter, i) of the block
-__device__ __forceinline__ int token_of(int quarter, int i) { return 4 * quarter + i % 4 + i / 4 * 16; }
+// nibble i of a quarter's value codes is token token_of(quarter, i) of the block
+__device__ __forceinline__ int token_of(int quarter, int i) {
+  return 4 * quarter + i % 4 + (i % 4 == 3 ? 1 - i / 4 : i / 4) * 16;
+}
 
 // this workgroup's block of the cache and the tokens of the call in it:
 // tokens [t0, t1) of the block are tokens from + (t - t0) of the sequence's rows
@@ -311,12 +327,12 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 //    keys), whose accumulators start from -16 sum q, and two multiply-adds in
 //    fp32; sum q is a constant of the loop.
 //  * softmax: a running maximum and sum per query, in fp32, one pass.
-//  * values: with P the weights and per group P' = P s_g,
-//      sum P v = sum P' (16 + c) - 16 sum P' + sum P m_g
+//  * values: with P the weights, per group P' = P s_g and b = 16 or 256 by the key,
+//      sum P v = sum P' (b + c) - sum b P' + sum P m_g
 //    the first sum by MFMA, the others in fp32 in the lane that holds P.  P' is
 //    rounded to fp16, in units of a 64th of the power of two above the largest
 //    s_g of the group so far (`unit` is the inverse), which keeps it in
-//    fp16's range whatever the values' size.  16 sum P' is of the rounded P', so
+//    fp16's range whatever the values' size.  sum b P' is of the rounded P', so
 //    that rounding costs 2^-12 of at most 15 s_g P a key, a quarter of a bf16
 //    result's own rounding.  (In bf16 it would be twice that rounding; hi and lo
 //    bf16 parts cost 12 instructions a row and group against 6.)
@@ -328,7 +344,7 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // Work is split over the keys: waves of a workgroup take every W-th block of
 // 32 keys, workgroups contiguous runs of them, joined in LDS and by
 // kv4_combine_kernel.
-// With R = 1 and dh = 128 a block is about 250 vector instructions and 16 MFMAs
+// With R = 1 and dh = 128 a block is about 210 vector instructions and 16 MFMAs
 // a wave against 5120 bytes.  A wave alone on its SIMD takes 0.8 us a block that
 // lies in cache and 1.2 from memory, two side by side 1.1 and 1.9: the memory
 // comes first.  156 registers leave three waves a SIMD; two took a third longer
@@ -453,7 +469,10 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   const uint8_t* const own = (const uint8_t*)a.cache + (size_t)bh * bytes;
   uint32_t* pw = lds[wave];
   const int prow = (c16 >> 2) * R + min(c16 & 3, R - 1);
-  const Unpack uk = Unpack::make<false>(), uv = Unpack::make<true>();
+  const UnpackKeys uk;
+  const UnpackValues uv;
+  // what the value operands of this lane's keys have above their codes, in 16ths
+  const f16x2 above = (c16 & 1) ? f16x2{(_Float16)16.f, (_Float16)16.f} : f16x2{(_Float16)1.f, (_Float16)1.f};
 
   Words<NG> kc[2], kp[2], vp[2];
   Words<ND> vc;
@@ -520,7 +539,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     for (int t = 0; t < 2; ++t) {
       f32x4 d[NG];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) d[g] = mfma(qa[g], __builtin_bit_cast(bf16x8, uk(kc[t].w[g])), q16[g]);
+      for (int g = 0; g < NG; ++g) d[g] = mfma(qa[g], uk(kc[t].w[g]), q16[g]);
       // keeps the unused rows' registers from being used again before the MFMAs are done
 #pragma unroll
       for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(d[g]));
@@ -606,7 +625,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     __builtin_amdgcn_wave_barrier();
     auto put = [&](int g, int r, float p0, float p1) {
       const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
-      psum[r][g] = __builtin_amdgcn_fdot2(h, f16x2{(_Float16)1.f, (_Float16)1.f}, psum[r][g], false);
+      psum[r][g] = __builtin_amdgcn_fdot2(h, above, psum[r][g], false);
       pw[(g * RT + kq * R + r) * 16 + c16] = __builtin_bit_cast(uint32_t, h);
     };
     if (whole) {
@@ -635,7 +654,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     for (int g = 0; g < NG; ++g) {
       const f16x8 ph = __builtin_bit_cast(f16x8, *(const u32x4*)&pw[(g * RT + prow) * 16 + kq * 4]);
 #pragma unroll
-      for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] = mfma(ph, __builtin_bit_cast(f16x8, uv(vc.w[d])), o[d]);
+      for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] = mfma(ph, uv(vc.w[d]), o[d]);
     }
     __builtin_amdgcn_sched_barrier(0);
     fetch_values(j + W);
@@ -755,7 +774,7 @@ struct Plan {
 // 0.5% slower than the fastest on average and 7% at most.  Smaller tiles than
 // the queries need unpack the cache again for each, but where whole ones leave
 // CUs idle they are faster: 16 sequences of 12 queries over 8 heads and a window
-// of 1024, one tile 13.5 us, two 10.2.
+// of 1024, one tile 13.5 us, two 10.1.
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
   Plan p{};
