@@ -554,3 +554,20 @@ def test_steps_that_fall_between_two_bf16_numbers():
     vb.vla_op_kv4_load(cache, 128, None, None, a, b)
     want = ref.bf16(ref.cached(k))
     assert np.array_equal(ref.from_dev(a), want) and np.array_equal(ref.from_dev(b), want)
+
+
+@pytest.mark.parametrize("B,Lq,max_len,lens", [(2, 1, 0, 0), (2, 1, 0, 9), (1, 5, 3, 3), (300, 1, 40, 37), (3, 70, 64, 64)])
+def test_attention_at_the_ends_of_its_sizes(B, Lq, max_len, lens):
+    """No tokens at all, a cut to none, more queries than tokens, many sequences."""
+    from paper_2608_14586_amd import binding as vb
+    H, Hkv, dh = 4, 2, 64
+    n = min(lens, max_len)
+    k, v = _kv(("ends", B, Lq), B, 64, Hkv, dh)
+    cache = _cache(B, Hkv, 64, dh, 255)
+    vb.vla_op_kv4_store(ref.to_dev(k), ref.to_dev(v), None, _i32(*[n] * B), cache, 64)
+    q = ref.normal(("endsq", B, Lq), (B, Lq, H, dh))
+    got = _attend(ref.to_dev(q), cache, 64, Hkv, [lens] * B, max_len)
+    if n == 0:
+        assert (got == 0).all()
+    else:
+        _check(got, q, k[:, :n], v[:, :n], [n] * B, 0, 0)
