@@ -23,6 +23,10 @@
 // hold two nibbles: at bits 6-9 of 16.0 one is 16 + c, at bits 2-5 of 256.0 it is
 // 256 + c, so one rotate by 8 serves all four pairs: 5 instructions a word in
 // place of 7, 1 to 3% of attention's time.
+#include <limits.h>
+
+#include <type_traits>
+
 #include "kernels.h"
 
 namespace vla {
@@ -31,12 +35,14 @@ namespace {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t ONES = 0x3f803f80u;  // bf16 1.0 twice
 constexpr int BLK = 32;  // tokens per block
 constexpr float LOWEST = -3e38f;  // a maximum before any score: finite, so that no difference of two is NaN
-constexpr float RAISE = 8.f;  // log2 by which a weight may exceed 1
-constexpr float UNIT = 64.f;  // what a step is at most as fp16: with RAISE 2^14, which leaves the small weights the most bits
+constexpr float RAISE = 8.f;  // log2 by which scores may rise before the maximum follows
+// exponents: P' as fp16 stays below 2^MOST, and the largest is put below 2^PLACE where it does not
+constexpr int MOST = 15, PLACE = 7;
 constexpr int KROT = 3, VROT = 6;
 __host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
 
@@ -330,12 +336,15 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 //  * values: with P the weights, per group P' = P s_g and b = 16 or 256 by the key,
 //      sum P v = sum P' (b + c) - sum b P' + sum P m_g
 //    the first sum by MFMA, the others in fp32 in the lane that holds P.  P' is
-//    rounded to fp16, in units of a 64th of the power of two above the largest
-//    s_g of the group so far (`unit` is the inverse), which keeps it in
-//    fp16's range whatever the values' size.  sum b P' is of the rounded P', so
-//    that rounding costs 2^-12 of at most 15 s_g P a key, a quarter of a bf16
-//    result's own rounding.  (In bf16 it would be twice that rounding; hi and lo
-//    bf16 parts cost 12 instructions a row and group against 6.)
+//    rounded to fp16, in a unit of each query and group of its own: a power of
+//    two that puts the largest P' of the keys so far that this query sees between
+//    2^6 and 2^15.  So a key weighs in a query's unit by what it adds to that query, and
+//    one that the query does not see, or gives no weight, moves nothing, however
+//    large its values.  sum b P' is of the rounded P', so that rounding costs 2^-11
+//    of at most 15 s_g P a key, half a bf16 result's own rounding of such a
+//    value, and less than 2^-31 of the largest P' where P' is subnormal.  (In
+//    bf16 it would be eight times that; hi and lo bf16 parts cost 12 instructions a
+//    row and group against 6.)
 // The 4 R queries of a tile sit in the MFMA rows 4 i + r, r < R, so with up to
 // four of them a lane holds one useful score a key and not four (R = 1).
 // P crosses from score lanes (one key each) to operand lanes (8 keys of one
@@ -398,6 +407,14 @@ __device__ __forceinline__ Words<N> load_words(__amdgpu_buffer_rsrc_t r, uint32_
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// the largest of a row's 16 lanes, as whole numbers
+__device__ __forceinline__ uint32_t row_max_u(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, true));
+}
+
 // 1 / x of a power of two from 2^-126 to 2^126
 __device__ __forceinline__ float inverse2(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 
@@ -456,13 +473,13 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   const int j0 = split * a.chunk, j1 = min(sn.nb, j0 + a.chunk);
   if (j0 >= sn.nb && split) return;
 
-  // this lane's rows of results: the positions of the first and last key that each sees in its window
-  int last[R], first[R];
+  // this lane's rows of results: the positions of the last key that each sees, and how far back it sees
+  int last[R];
+  const int span = a.window ? a.window : INT_MAX;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = row0 + kq * R + r;
     last[r] = row < rows ? len - a.Lq + div_by(row, a.by_G) : -1;
-    first[r] = a.window ? last[r] - a.window + 1 : 0;
   }
   // the blocks of this sequence and head (at most 2^24 tokens: below 2^32 bytes)
   const uint32_t bytes = (uint32_t)(a.L_cap / BLK) * (40 * DH);
@@ -478,25 +495,26 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   Words<ND> vc;
   auto block_of = [&](int j) { return j < sn.sinkb ? j : sn.blk0 + j - sn.sinkb; };
   // past the run's last block the buffer is empty and the loads touch no memory:
-  // a branch around them would make every wait one for all loads
+  // a branch around them would make every wait one for all loads.  What a load has
+  // beyond its lane's own offset goes into the wave's: it costs no registers there
+  auto there = [&](int j) { return (uint32_t)((j - j1) >> 31); };  // all bits, or none
   auto buffer = [&](int j) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)own, (short)0, j < j1 ? (int)bytes : 0, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)own, (short)0, (int)(bytes & there(j)), 0x00020000);
   };
+  auto part_of = [&](int j, uint32_t at) { return ((uint32_t)block_of(j) * (40 * DH) + at) & there(j); };
   auto fetch_keys = [&](int j) {
-    const uint32_t base = j < j1 ? (uint32_t)block_of(j) * (40 * DH) : 0;
     const __amdgpu_buffer_rsrc_t cache = buffer(j);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      kc[t] = load_words<NG>(cache, t * 8 * DH + c16 * (DH / 2) + kq * (DH / 8), base);
-      kp[t] = load_words<NG>(cache, 32 * DH + (t * 16 + c16) * NG * 4, base);
+      kc[t] = load_words<NG>(cache, t * 8 * DH + c16 * (DH / 2) + kq * (DH / 8), part_of(j, 0));
+      kp[t] = load_words<NG>(cache, (t * 16 + c16) * NG * 4, part_of(j, 32 * DH));
     }
   };
   auto fetch_values = [&](int j) {
-    const uint32_t base = j < j1 ? (uint32_t)block_of(j) * (40 * DH) : 0;
     const __amdgpu_buffer_rsrc_t cache = buffer(j);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) vp[t] = load_words<NG>(cache, 36 * DH + (t * 16 + c16) * NG * 4, base);
-    vc = load_words<ND>(cache, 16 * DH + lane * ND * 4, base);
+    for (int t = 0; t < 2; ++t) vp[t] = load_words<NG>(cache, (t * 16 + c16) * NG * 4, part_of(j, 36 * DH));
+    vc = load_words<ND>(cache, lane * ND * 4, part_of(j, 16 * DH));
   };
   // the next block's keys and values are on their way as soon as this block's are used up
   fetch_keys(j0 + wave);
@@ -507,34 +525,37 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
 #pragma unroll
   for (int g = 0; g < NG; ++g) qa[g] = __builtin_bit_cast(bf16x8, qw[g]);
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  // the sums of each query's groups, and -16 times them: where the scores' accumulators start
+  // the sums of each query's groups, and -16 times them: where the scores' accumulators
+  // start.  With R = 4 the registers of the former are wanted: 8 products a block in their place
+  constexpr bool KEEP = R < 4;
   f32x4 q16[NG];
-  float qs[NG][R];
+  float qs[NG][KEEP ? R : 1];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     q16[g] = mfma(qa[g], __builtin_bit_cast(bf16x8, u32x4{0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u}), zero);
 #pragma unroll
-    for (int r = 0; r < R; ++r) qs[g][r] = -0.0625f * q16[g][r];
+    for (int r = 0; KEEP && r < R; ++r) qs[g][r] = -0.0625f * q16[g][r];
   }
 
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zero;
-  float m[R], l[R], bias[R][NG], psum[R][NG], unit[NG];  // sums of P, P m and P' of this lane's keys
-#pragma unroll
-  for (int g = 0; g < NG; ++g) unit[g] = 0x1p126f;  // every step but 0 exceeds it
+  float m[R], l[R], bias[R][NG], psum[R][NG], unit[R][NG];  // sums of P, P m and P' of this lane's keys
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = LOWEST;
     l[r] = 0.f;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) bias[r][g] = psum[r][g] = 0.f;
+    for (int g = 0; g < NG; ++g) {
+      bias[r][g] = psum[r][g] = 0.f;
+      unit[r][g] = 0x1p126f;
+    }
   }
   for (int j = j0 + wave; j < j1; j += W) {
     const int key0 = block_of(j) * BLK;
     // every row sees the whole block
     const bool whole = key0 + BLK - 1 <= sn.pos0 && (!a.window || key0 > sn.pos1 - a.window);
-    float p[2][R];
+    float sc[2][R];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       f32x4 d[NG];
@@ -544,19 +565,21 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
 #pragma unroll
       for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(d[g]));
 #pragma unroll
-      for (int r = 0; r < R; ++r) p[t][r] = 0.f;
+      for (int r = 0; r < R; ++r) sc[t][r] = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const float low = hi16(kp[t].w[g]) * (KEEP ? 1.f : -0.0625f);
+#pragma unroll
+        for (int r = 0; r < R; ++r) sc[t][r] = fmaf(low, KEEP ? qs[g][r] : q16[g][r], sc[t][r]);
+      }
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int r = 0; r < R; ++r) p[t][r] = fmaf(hi16(kp[t].w[g]), qs[g][r], p[t][r]);
-#pragma unroll
-      for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int r = 0; r < R; ++r) p[t][r] = fmaf(lo16(kp[t].w[g]), d[g][r], p[t][r]);
+        for (int r = 0; r < R; ++r) sc[t][r] = fmaf(lo16(kp[t].w[g]), d[g][r], sc[t][r]);
     }
     // no use of this block's registers may sink below the loads into them
 #pragma unroll
-    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(p[0][r]), "+v"(p[1][r]));
+    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(sc[0][r]), "+v"(sc[1][r]));
     __builtin_amdgcn_sched_barrier(0);
     fetch_keys(j + W);
     if (!whole) {
@@ -566,95 +589,106 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
         // also replaces whatever the cache's unwritten rows gave
 #pragma unroll
         for (int r = 0; r < R; ++r)
-          p[t][r] = (key <= last[r]) & ((key >= first[r]) | (key < a.sinks)) ? p[t][r] : -INFINITY;
-        // what a row that nobody sees holds must not choose the unit: its step becomes 0
-        const bool seen = (key <= sn.pos1) & (!a.window | (key > sn.pos0 - a.window) | (key < a.sinks));
-#pragma unroll
-        for (int g = 0; g < NG; ++g) vp[t].w[g] &= seen ? 0xffffffffu : 0xffff0000u;
+          sc[t][r] = (key <= last[r]) & ((last[r] - key < span) | (key < a.sinks)) ? sc[t][r] : -INFINITY;
       }
     }
-    float vs[2][NG];
+    // The weights, P' as fp16 pairs, and whether this lane has one past its range: a
+    // score above m, or a P' of 2^MOST and more (both halves of a pair at once)
+    float p[2][R];
+    uint32_t ph[R][NG];
+    auto weigh = [&](auto all) {
+      // what the two calls and the rescaling have in common would be kept in between:
+      // registers that nothing has left (a third of a wave's at R = 4)
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int g = 0; g < NG; ++g) vs[t][g] = lo16(vp[t].w[g]) * unit[g];
-    // the running maximum moves only where a score exceeds it by RAISE, and
-    // the unit of a group's steps only where a step exceeds it, so most blocks
-    // rescale nothing, and a lane asks for its own keys alone
-    bool raise = false;
-#pragma unroll
-    for (int r = 0; r < R; ++r) raise |= fmaxf(p[0][r], p[1][r]) * a.scale_log2 > m[r] + RAISE;
-    float most = fmaxf(vs[0][0], vs[1][0]);
-#pragma unroll
-    for (int g = 1; g < NG; ++g) most = fmaxf(most, fmaxf(vs[0][g], vs[1][g]));
-    if (__any(raise || most > UNIT)) {
-      float f[NG];  // what the group's unit changes by
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        // UNIT / unit: the power of two above the largest step so far
-        const float s0 = lo16(vp[0].w[g]), s1 = lo16(vp[1].w[g]);
-        const uint32_t e = __float_as_uint(row_max<>(fmaxf(s0, s1))) & 0x7f800000u;
-        const float u = fminf(unit[g], e && e < 0x7f800000u ? UNIT * __uint_as_float(0x7e800000u - e) : 0x1p126f);
-        f[g] = u * inverse2(unit[g]);
-        unit[g] = u;
-        vs[0][g] = s0 * u;
-        vs[1][g] = s1 * u;
-      }
+      for (int r = 0; r < R; ++r) asm("" : "+v"(sc[0][r]), "+v"(sc[1][r]));
+      bool past = false;
+      u16x2 most = {0, 0};
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const float mn = fmaxf(m[r], row_max<>(fmaxf(p[0][r], p[1][r])) * a.scale_log2);
-        const float al = exp2_of(m[r] - mn);
-        m[r] = mn;
-        l[r] *= al;
+        p[0][r] = exp2_of(fmaf(sc[0][r], a.scale_log2, -m[r]));
+        p[1][r] = exp2_of(fmaf(sc[1][r], a.scale_log2, -m[r]));
+        past |= fmaxf(p[0][r], p[1][r]) > 1.f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          bias[r][g] *= al;
-          psum[r][g] *= al * f[g];
+          float x0 = p[0][r] * lo16(vp[0].w[g]) * unit[r][g], x1 = p[1][r] * lo16(vp[1].w[g]) * unit[r][g];
+          if constexpr (!all.value) {  // a key that the row does not see may hold NaN
+            x0 = p[0][r] == 0.f ? 0.f : x0;
+            x1 = p[1][r] == 0.f ? 0.f : x1;
+          }
+          const u16x2 h = __builtin_bit_cast(u16x2, __builtin_convertvector((f32x2{x0, x1}), f16x2));
+          most = __builtin_elementwise_max(most, h);
+          ph[r][g] = __builtin_bit_cast(uint32_t, h);
         }
-#pragma unroll
-        for (int d = 0; d < ND; ++d) o[d][r] *= al * f[d / 2];
       }
-    }
+      return past || ((__builtin_bit_cast(uint32_t, most) + 0x08000800u) & 0x80008000u);
+    };
+    auto weigh_block = [&] { return whole ? weigh(std::true_type{}) : weigh(std::false_type{}); };
+    // The maximum moves where a score exceeds it, and then RAISE above the score, and
+    // a unit where a P' passes its range: in a wave's first block, and in few others.
+    // What a row does here goes by its own scores and P' alone, so its result does not
+    // depend on the tile's other rows.  Exponents are fp32's, 127 for 2^0.
+    bool some = j == j0 + wave;
+    if (!some) some = __any(weigh_block());
+    if (some) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      p[0][r] = exp2_of(fmaf(p[0][r], a.scale_log2, -m[r]));
-      p[1][r] = exp2_of(fmaf(p[1][r], a.scale_log2, -m[r]));
-      l[r] += p[0][r] + p[1][r];
+      for (int r = 0; r < R; ++r) {
+        const float top = row_max<>(fmaxf(sc[0][r], sc[1][r])) * a.scale_log2;
+        const bool up = top > m[r];
+        const float mn = up ? ceilf(top) + RAISE : m[r];  // whole numbers: what came before shrinks by 2^down
+        const int down = up ? (int)fminf(mn - m[r], 512.f) : 0;
+        m[r] = mn;
+        l[r] = ldexpf(l[r], -down);
+        const float p0 = exp2_of(fmaf(sc[0][r], a.scale_log2, -mn)), p1 = exp2_of(fmaf(sc[1][r], a.scale_log2, -mn));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          // the largest P s; NaN, as of unseen keys (0 times anything), is none
+          const float x = fmaxf(fmaxf(p0 * lo16(vp[0].w[g]), p1 * lo16(vp[1].w[g])), 0.f);
+          const int ex = (int)(row_max_u(__float_as_uint(x)) >> 23), e0 = (int)(__float_as_uint(unit[r][g]) >> 23);
+          const int e1 = min(e0 + down, 253);  // so its unit may grow as much
+          const int e = ex + e1 >= 254 + MOST ? 253 + PLACE - ex : e1;
+          const int f = e - e0 - down;
+          unit[r][g] = __uint_as_float((uint32_t)e << 23);
+          bias[r][g] = ldexpf(bias[r][g], -down);
+          psum[r][g] = ldexpf(psum[r][g], f);
+          o[2 * g][r] = ldexpf(o[2 * g][r], f);
+          o[2 * g + 1][r] = ldexpf(o[2 * g + 1][r], f);
+        }
+      }
+      weigh_block();
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of pw come first
     __builtin_amdgcn_wave_barrier();
-    auto put = [&](int g, int r, float p0, float p1) {
-      const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
-      psum[r][g] = __builtin_amdgcn_fdot2(h, above, psum[r][g], false);
-      pw[(g * RT + kq * R + r) * 16 + c16] = __builtin_bit_cast(uint32_t, h);
-    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      l[r] += p[0][r] + p[1][r];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        psum[r][g] = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, ph[r][g]), above, psum[r][g], false);
+        pw[(g * RT + kq * R + r) * 16 + c16] = ph[r][g];
+      }
+    }
     if (whole) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
+        for (int g = 0; g < NG; ++g)
           bias[r][g] = fmaf(p[0][r], hi16(vp[0].w[g]), fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]));
-          put(g, r, p[0][r] * vs[0][g], p[1][r] * vs[1][g]);
-        }
-    } else {  // a key that the row does not see may hold NaN
+    } else {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const bool s0 = p[0][r] != 0.f, s1 = p[1][r] != 0.f;
+      for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float b1 = s1 ? fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]) : bias[r][g];
-          bias[r][g] = s0 ? fmaf(p[0][r], hi16(vp[0].w[g]), b1) : b1;
-          put(g, r, s0 ? p[0][r] * vs[0][g] : 0.f, s1 ? p[1][r] * vs[1][g] : 0.f);
+          const float b1 = p[1][r] == 0.f ? bias[r][g] : fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]);
+          bias[r][g] = p[0][r] == 0.f ? b1 : fmaf(p[0][r], hi16(vp[0].w[g]), b1);
         }
-      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const f16x8 ph = __builtin_bit_cast(f16x8, *(const u32x4*)&pw[(g * RT + prow) * 16 + kq * 4]);
+      const f16x8 pa = __builtin_bit_cast(f16x8, *(const u32x4*)&pw[(g * RT + prow) * 16 + kq * 4]);
 #pragma unroll
-      for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] = mfma(ph, uv(vc.w[d]), o[d]);
+      for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] = mfma(pa, uv(vc.w[d]), o[d]);
     }
     __builtin_amdgcn_sched_barrier(0);
     fetch_values(j + W);
@@ -673,7 +707,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float w = inverse2(unit[g]), bs = row_sum<>(fmaf(-16.f * psum[r][g], w, bias[r][g]));
+      const float w = inverse2(unit[r][g]), bs = row_sum<>(fmaf(-16.f * psum[r][g], w, bias[r][g]));
 #pragma unroll
       for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = fmaf(o[d][r], w, bs);
     }
