@@ -612,8 +612,8 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
         for (int g = 0; g < NG; ++g) {
           float x0 = p[0][r] * lo16(vp[0].w[g]) * unit[r][g], x1 = p[1][r] * lo16(vp[1].w[g]) * unit[r][g];
           if constexpr (!all.value) {  // a key that the row does not see may hold NaN
-            x0 = p[0][r] == 0.f ? 0.f : x0;
-            x1 = p[1][r] == 0.f ? 0.f : x1;
+            x0 = sc[0][r] == -INFINITY ? 0.f : x0;
+            x1 = sc[1][r] == -INFINITY ? 0.f : x1;
           }
           const u16x2 h = __builtin_bit_cast(u16x2, __builtin_convertvector((f32x2{x0, x1}), f16x2));
           most = __builtin_elementwise_max(most, h);
@@ -678,8 +678,8 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float b1 = p[1][r] == 0.f ? bias[r][g] : fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]);
-          bias[r][g] = p[0][r] == 0.f ? b1 : fmaf(p[0][r], hi16(vp[0].w[g]), b1);
+          const float b1 = sc[1][r] == -INFINITY ? bias[r][g] : fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]);
+          bias[r][g] = sc[0][r] == -INFINITY ? b1 : fmaf(p[0][r], hi16(vp[0].w[g]), b1);
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

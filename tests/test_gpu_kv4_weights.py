@@ -146,6 +146,28 @@ def test_a_query_beside_one_that_is_not_finite():
         assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("n", [64, 70])
+def test_values_that_are_not_finite(n):
+    """A key that a query sees, of a weight that is 0 in fp32, with a value that is
+    not finite: NaN in that group of 32 dims, whether the key's block is seen whole or
+    in part, and in no other group; a query that does not see it is as without it."""
+    B, Lq, H, Hkv, dh = 1, 2, 4, 2, 128
+    for at in (3, n - 1):
+        k, v = _kv(("notfinite", n), B, n, Hkv, dh)
+        q = ref.normal(("notfiniteq", n), (B, Lq, H, dh))
+        k[..., 0], q[..., 0] = 0.0, 8.0
+        k[:, at, :, 0] = ref.bf16(-300.0 * np.sqrt(dh) / 8.0)
+        bad = v.copy()
+        bad[:, at, :, 40] = np.inf
+        cap = (n + 31) // 32 * 32
+        a = _attend(ref.to_dev(q), _stored(k, v, [n], cap), cap, Hkv, [n], n)
+        b = _attend(ref.to_dev(q), _stored(k, bad, [n], cap), cap, Hkv, [n], n)
+        sees = [0, 1] if at == 3 else [1]
+        assert np.isnan(b[0, sees][..., 32:64]).all()
+        b[0, sees, :, 32:64] = a[0, sees, :, 32:64]
+        assert np.array_equal(a, b)
+
+
 # Sizes at which the call takes 4, 8 and 16 queries a tile, 4 and 8 waves, one split,
 # several, and more than the 64 that are joined at a time; no number of query
 # rows is a multiple of the tile's.  The last column: blocks a wave takes at most.
