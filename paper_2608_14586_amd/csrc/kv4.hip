@@ -707,9 +707,10 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float w = inverse2(unit[r][g]), bs = row_sum<>(fmaf(-16.f * psum[r][g], w, bias[r][g]));
+      // the difference first: it is no larger than the values are
+      const float w = inverse2(unit[r][g]), bs = row_sum<>(bias[r][g]), ps = row_sum<>(psum[r][g]);
 #pragma unroll
-      for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = fmaf(o[d][r], w, bs);
+      for (int d = 2 * g; d < 2 * g + 2; ++d) ow[row * DH + d * 16 + c16] = fmaf(fmaf(-16.f, ps, o[d][r]), w, bs);
     }
   }
   __syncthreads();

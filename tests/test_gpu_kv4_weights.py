@@ -168,6 +168,35 @@ def test_values_that_are_not_finite(n):
         assert np.array_equal(a, b)
 
 
+@pytest.mark.parametrize("n", [1, 2, 40])
+def test_the_largest_values(n):
+    """Values whose steps reach 2^124: the weighted sums stay in fp32."""
+    B, H, Hkv, dh = 1, 4, 2, 64
+    k, v = _kv(("largest", n), B, n, Hkv, dh)
+    v = ref.bf16(np.sign(v) * 2.0 ** 127)
+    q = ref.normal(("largestq", n), (B, 1, H, dh))
+    cap = (n + 31) // 32 * 32
+    got = _attend(ref.to_dev(q), _stored(k, v, [n], cap), cap, Hkv, [n], n)
+    assert np.isfinite(got).all()
+    _check(got, q, k, v, [n])
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_the_largest_value_behind_others(dh):
+    """A key whose score is up to 2^8 above those seen before it, so that it moves no
+    maximum, with values of 2^127: its weight is nearly 1 there, and 256 steps
+    of it would not be finite."""
+    B, H, Hkv, n = 1, 8, 1, 600  # three blocks of 32 for each of eight waves
+    k, v = _kv(("behind", dh), B, n, Hkv, dh)
+    q = ref.normal(("behindq", dh), (B, 1, H, dh), 0.1)
+    k[..., 0], q[..., 0] = 0.0, 8.0
+    k[:, 301, :, 0] = ref.bf16(5.0 * np.sqrt(dh) / 8.0)
+    v[:, 301] = ref.bf16(np.sign(v[:, 301]) * 2.0 ** 127)
+    got = _attend(ref.to_dev(q), _stored(k, v, [n], 608), 608, Hkv, [n], n)
+    assert np.isfinite(got).all()
+    _check(got, q, k, v, [n])
+
+
 # Sizes at which the call takes 4, 8 and 16 queries a tile, 4 and 8 waves, one split,
 # several, and more than the 64 that are joined at a time; no number of query
 # rows is a multiple of the tile's.  The last column: blocks a wave takes at most.
