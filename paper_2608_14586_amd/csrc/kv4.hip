@@ -43,6 +43,7 @@ constexpr float LOWEST = -3e38f;  // a maximum before any score: finite, so that
 constexpr float RAISE = 8.f;  // log2 by which scores may rise before the maximum follows
 // exponents: P' as fp16 stays below 2^MOST, and the largest is put below 2^PLACE where it does not
 constexpr int MOST = 15, PLACE = 7;
+constexpr float MID = 7.5f;  // of the codes
 constexpr int KROT = 3, VROT = 6;
 __host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
 
@@ -334,17 +335,18 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 //    fp32; sum q is a constant of the loop.
 //  * softmax: a running maximum and sum per query, in fp32, one pass.
 //  * values: with P the weights, per group P' = P s_g and b = 16 or 256 by the key,
-//      sum P v = sum P' (b + c) - sum b P' + sum P m_g
+//      sum P v = sum P' (b + c) - sum (b + 7.5) P' + sum P (m_g + 7.5 s_g)
 //    the first sum by MFMA, the others in fp32 in the lane that holds P.  P' is
 //    rounded to fp16, in a unit of each query and group of its own: a power of
 //    two that puts the largest P' of the keys so far that this query sees between
 //    2^6 and 2^15.  So a key weighs in a query's unit by what it adds to that query, and
 //    one that the query does not see, or gives no weight, moves nothing, however
-//    large its values.  sum b P' is of the rounded P', so that rounding costs 2^-11
-//    of at most 15 s_g P a key, half a bf16 result's own rounding of such a
-//    value, and less than 2^-31 of the largest P' where P' is subnormal.  (In
-//    bf16 it would be eight times that; hi and lo bf16 parts cost 12 instructions a
-//    row and group against 6.)
+//    large its values.  The second sum is of the rounded P', so that rounding costs
+//    2^-11 of at most 7.5 s_g P a key, a quarter of a bf16 result's own rounding of
+//    15 s_g P, and less than 2^-31 of the largest P' where P' is subnormal.  (Without the
+//    7.5, the middle of the codes, it would be twice that, for 8 of 215 instructions; in
+//    bf16 eight times; hi and lo bf16 parts cost 12 instructions a row and group
+//    against 6.)
 // The 4 R queries of a tile sit in the MFMA rows 4 i + r, r < R, so with up to
 // four of them a lane holds one useful score a key and not four (R = 1).
 // P crosses from score lanes (one key each) to operand lanes (8 keys of one
@@ -488,8 +490,9 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   const int prow = (c16 >> 2) * R + min(c16 & 3, R - 1);
   const UnpackKeys uk;
   const UnpackValues uv;
-  // what the value operands of this lane's keys have above their codes, in 16ths
-  const f16x2 above = (c16 & 1) ? f16x2{(_Float16)16.f, (_Float16)16.f} : f16x2{(_Float16)1.f, (_Float16)1.f};
+  // what the value operands of this lane's keys have above their codes, and MID, in 16ths
+  const _Float16 over = (_Float16)((c16 & 1 ? 256 + MID : 16 + MID) / 16);
+  const f16x2 above = {over, over};
 
   Words<NG> kc[2], kp[2], vp[2];
   Words<ND> vc;
@@ -667,19 +670,24 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
         pw[(g * RT + kq * R + r) * 16 + c16] = ph[r][g];
       }
     }
+    float mid[2][NG];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) mid[t][g] = fmaf(MID, lo16(vp[t].w[g]), hi16(vp[t].w[g]));
     if (whole) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int g = 0; g < NG; ++g)
-          bias[r][g] = fmaf(p[0][r], hi16(vp[0].w[g]), fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]));
+          bias[r][g] = fmaf(p[0][r], mid[0][g], fmaf(p[1][r], mid[1][g], bias[r][g]));
     } else {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float b1 = sc[1][r] == -INFINITY ? bias[r][g] : fmaf(p[1][r], hi16(vp[1].w[g]), bias[r][g]);
-          bias[r][g] = sc[0][r] == -INFINITY ? b1 : fmaf(p[0][r], hi16(vp[0].w[g]), b1);
+          const float b1 = sc[1][r] == -INFINITY ? bias[r][g] : fmaf(p[1][r], mid[1][g], bias[r][g]);
+          bias[r][g] = sc[0][r] == -INFINITY ? b1 : fmaf(p[0][r], mid[0][g], b1);
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

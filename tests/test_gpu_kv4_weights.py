@@ -16,14 +16,14 @@ def attention_and_bound(q, k, v, length, window, sinks, steps=None):
     a result may be off.  Per query, head and group of 32 dims, with p the softmax
     weights, s and m a key's step and minimum in the cache:
       - the result's rounding to bf16: 2^-8 of it;
-      - the rounding of p s to fp16, half a step or 2^-11 of it, times a code of at
-        most 15: 2^-11 * 15 sum p s;
+      - the rounding of p s to fp16, half a step or 2^-11 of it, times a code counted
+        from the middle: 2^-11 * 7.5 sum p s;
       - scores: a group's sum of (16 + c) q starts from -16 sum q, 47 sum |q| in all,
         and takes m sum q: 34 fp32 roundings for the sums and two a group where the
         groups are joined, each at most 2^-24 of sum_g (47 s + |m|) sum |q|; then two
         of the score itself (2^-23), and the exponential (2^-21).  A weight's relative
         error e moves the result by p e (|v| + |o|);
-      - sums over keys in fp32: of p s (b + c) and p s b, each at most 271 p s, one
+      - sums over keys in fp32: of p s (b + c) and p s (b + 7.5), each at most 271 p s, one
         rounding a block and 32 in it, and of p m, two a block; 100 more to join
         waves and splits.  `steps`: how many blocks a wave takes at most."""
     Lq, H, dh = q.shape
@@ -51,7 +51,7 @@ def attention_and_bound(q, k, v, length, window, sinks, steps=None):
             assert (err < 0.1).all()  # e^x - 1 <= 1.1 x
             ps = np.repeat(p @ sv[at][..., 0], 32, -1)
             e = (p * err) @ np.abs(vv[at]) + (p * err).sum(-1, keepdims=True) * np.abs(y)
-            e += 2.0 ** -11 * 15 * ps
+            e += 2.0 ** -11 * 7.5 * ps
             e += 2.0 ** -24 * ((steps + 132) * 542 * ps + (2 * steps + 132) * (p @ mag[at]))
             o[i, h * G:(h + 1) * G] = y
             bound[i, h * G:(h + 1) * G] = 2.0 ** -8 * np.abs(y) + (1 + 2.0 ** -7) * e + 2.0 ** -126
@@ -195,6 +195,24 @@ def test_the_largest_value_behind_others(dh):
     got = _attend(ref.to_dev(q), _stored(k, v, [n], 608), 608, Hkv, [n], n)
     assert np.isfinite(got).all()
     _check(got, q, k, v, [n])
+
+
+@pytest.mark.parametrize("Lq,n", [(1, 1), (3, 3), (1, 2), (1, 40)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_rounding_of_the_weights(Lq, n, dh):
+    """Values of 0 in groups of a minimum -15 a and step a = 1, so that the result is 0 and
+    nothing but the rounding of p s shows: at most 2^-11 * 7.5 sum p s, the codes
+    counted from their middle, and less than 2^-10 from the sums in fp32 (at most
+    279 sum p s, 44 roundings of 2^-24)."""
+    B, H, Hkv = 1, 64, 1
+    k, _ = _kv(("rounding", dh, n), B, n, Hkv, dh)
+    q = ref.normal(("roundingq", dh, n), (B, Lq, H, dh))
+    v = np.zeros((B, n, Hkv, dh))
+    v[..., ::32] = -15.0
+    got = _attend(ref.to_dev(q), _stored(k, v, [n], 64), 64, Hkv, [n], n)
+    got = got.reshape(Lq, H, dh // 32, 32)
+    assert (np.abs(got[..., 0] + 15) <= 2.0 ** -8 * 15).all()
+    assert (np.abs(got[..., 1:]) <= (1 + 2.0 ** -8) * (2.0 ** -11 * 7.5 + 2.0 ** -10)).all()
 
 
 # Sizes at which the call takes 4, 8 and 16 queries a tile, 4 and 8 waves, one split,
