@@ -175,8 +175,10 @@ vla_status vla_op_kv4_load(const void *cache, const int32_t *start, const int32_
  * below 0, are cut), max_len <= L_cap; it decides how the work is split, so
  * the closer the better.  scratch: vla_op_attention_kv4_scratch bytes (may be
  * 0) of device memory, 16-byte aligned, for this call alone until it is done
- * (calls that may run at the same time need one each).  VLA_ERR_SHAPE if
- * scratch_bytes is less.  dh in {64, 128}, H % Hkv == 0. */
+ * (calls that may run at the same time need one each).  That size never falls
+ * with max_len, all else alike: scratch for the longest call serves every
+ * shorter one.  VLA_ERR_SHAPE if scratch_bytes is less.  dh in {64, 128}, H %
+ * Hkv == 0. */
 size_t vla_op_attention_kv4_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
 vla_status vla_op_attention_kv4(const vla_heads *q, const void *cache, const int32_t *lens, const vla_heads *o, int B,
                                 int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,

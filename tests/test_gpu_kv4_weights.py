@@ -249,3 +249,20 @@ def test_windows_of_several_queries(B, Lq, H, Hkv, n, window, sinks):
     cap = (n + 31) // 32 * 32
     got = _attend(ref.to_dev(q), _stored(k, v, lens, cap), cap, Hkv, lens, n, window, sinks)
     _check(got, q, k, v, lens, window, sinks)
+
+
+@pytest.mark.parametrize("B,Lq,H,Hkv,dh,longest", [(8, 1, 32, 8, 128, 1000), (3, 4, 8, 8, 64, 2048)])
+def test_one_scratch_for_a_growing_length(B, Lq, H, Hkv, dh, longest):
+    """Scratch sized once, for the longest call, serves every shorter one."""
+    import torch
+    from paper_2608_14586_amd import binding as vb
+    k, v = _kv(("growing", dh), B, longest, Hkv, dh)
+    q = ref.normal(("growingq", dh), (B, Lq, H, dh))
+    cache = _stored(k, v, [longest] * B, longest + 31 & ~31)
+    scratch = torch.empty(vb.vla_op_attention_kv4_scratch(B, Lq, H, Hkv, dh, longest), dtype=torch.uint8, device="cuda")
+    dq, o = ref.to_dev(q), torch.empty((B, Lq, H, dh), dtype=torch.bfloat16, device="cuda")
+    for n in (Lq, 37, 130, 500, longest * 15 // 16, longest):
+        scratch.fill_(255)
+        lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+        vb.vla_op_attention_kv4(dq, cache, longest + 31 & ~31, Hkv, lens, o, n, 0, 0, scratch)
+        _check(ref.from_dev(o), q, k, v, [n] * B)
