@@ -416,7 +416,9 @@ def vla_op_gemm_tile_bf16(op, tile, A, Wp, out, bias, M, N, K, stream=None):
 # These calls take torch tensors on the GPU and read sizes and strides off
 # them (csrc/torch_ops.cpp); a tensor whose type, shape, device or size does
 # not fit raises ValueError before the library is called.  `stream`: a
-# hipStream_t (torch's `stream.cuda_stream`), None = the null stream.
+# hipStream_t (torch's `stream.cuda_stream`), None = torch's current stream, so
+# that a call comes after what made its tensors and is captured with it.  (The
+# calls above take addresses, and None is the null stream there.)
 
 _torch_ops = None
 

@@ -87,7 +87,7 @@ def build(verbose: bool = False) -> str:
         objs = list(ex.map(_compile, SOURCES))
     _link([HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC"] + objs, LIB)
     _link(["g++", "-shared", torch_obj.result(), "-L" + HERE, "-lvlaprefix", "-Wl,-rpath,$ORIGIN",
-           "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], TORCH_OPS)
+           "-L" + os.path.join(_torch_dir(), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"], TORCH_OPS)
     if verbose:
         print("built", LIB)
     return LIB

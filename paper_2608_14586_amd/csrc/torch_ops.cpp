@@ -8,6 +8,7 @@
 // for a tensor whose type, shape, device or size does not fit.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
 
 #include "../../include/vla_ops.h"
@@ -68,8 +69,9 @@ int int_of(PyObject* o, const char* name) {
   }
   return (int)v;
 }
+// None: torch's current stream of the current device, where its tensors' work is
 void* stream_of(PyObject* o) {
-  if (o == Py_None) return nullptr;
+  if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
   void* s = PyLong_AsVoidPtr(o);
   if (!s && PyErr_Occurred()) {
     PyErr_Clear();
