@@ -156,6 +156,11 @@ vla_status qk_norm_rope(PyObject* const* a) {
     n_pos = dim(c, 0, "cos");
   }
   const int64_t ts[2] = {n_pos, dh / 2};
+  // a table without rows has no address, and none at all means no rotation: any address, never read, stands for it
+  auto table = [&](PyObject* o, const char* name) {
+    void* p = dense(o, F32, ts, dev, name);
+    return (const float*)(o != Py_None && n_pos == 0 ? qh.p : p);
+  };
   const double eps = PyFloat_AsDouble(a[4]);
   if (eps == -1.0 && PyErr_Occurred()) {
     PyErr_Clear();
@@ -163,7 +168,7 @@ vla_status qk_norm_rope(PyObject* const* a) {
   }
   return vla_op_qk_norm_rope(&qh, &kh, type == F32 ? VLA_F32 : VLA_BF16, (float*)dense(a[2], F32, gs, dev, "gq"),
                              (float*)dense(a[3], F32, gs, dev, "gk"), (float)eps,
-                             (float*)dense(a[5], F32, ts, dev, "cos"), (float*)dense(a[6], F32, ts, dev, "sin"), n_pos,
+                             table(a[5], "cos"), table(a[6], "sin"), n_pos,
                              (int32_t*)dense(a[7], I32, ps, dev, "pos"), &qo, &ko, B, L, H, Hkv, dh, stream_of(a[10]));
 }
 
