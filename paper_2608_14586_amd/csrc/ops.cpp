@@ -178,7 +178,8 @@ vla_status vla_op_gemv_w4(const void* x, int64_t ldx, const void* Wp, const floa
       !aligned(residual, 4) || (swiglu && N % 32))
     return VLA_ERR_UNSUPPORTED;
   if (M > 1 && (ldx < K || ldo < (swiglu ? N / 2 : N))) return VLA_ERR_INVALID_ARG;
-  if (M > 16 * 65535 || (M > 1 && (15 * ldx + K) * 2 >= (int64_t)1 << 31)) return VLA_ERR_UNSUPPORTED;
+  // 16 rows of x lie within 2^31 bytes
+  if (M > 16 * 65535 || (M > 1 && ldx > ((1 << 30) - 1 - K) / 15)) return VLA_ERR_UNSUPPORTED;
   if (M == 0) return VLA_OK;
   return status_of(vla::gemv_w4((const bf16_t*)x, ldx, Wp, residual, out, ldo, out_dtype == VLA_F32, swiglu != 0, M, N,
                                 K, group, (hipStream_t)stream));
