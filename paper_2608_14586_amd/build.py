@@ -54,7 +54,11 @@ def _compile(src: str) -> str:
 
 
 def _torch_dir() -> str:
-    return list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("_torch_ops.so, the 4-bit operators on torch tensors, needs torch's headers and libraries, "
+                           "and torch is not installed (libvlaprefix.so does without)")
+    return list(spec.submodule_search_locations)[0]
 
 
 def _compile_torch_ops() -> str:
@@ -64,7 +68,10 @@ def _compile_torch_ops() -> str:
     cmd = ["g++", "-D__HIP_PLATFORM_AMD__"] + HOST_FLAGS + \
         ["-I" + d for d in (inc, os.path.join(inc, "torch", "csrc", "api", "include"), "/opt/rocm/include",
                             sysconfig.get_paths()["include"])] + ["-c", os.path.join(CSRC, "torch_ops.cpp"), "-o", obj]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except FileNotFoundError:
+        raise RuntimeError("_torch_ops.so, the 4-bit operators on torch tensors, needs g++ (libvlaprefix.so does without)")
     if r.returncode != 0:
         raise RuntimeError("g++ failed for torch_ops.cpp:\n%s\n%s" % (" ".join(cmd), r.stderr[-6000:]))
     return obj
@@ -79,8 +86,9 @@ def _link(cmd, out: str) -> None:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source and link the shared library and the module of torch
-    calls; returns the library's path."""
+    """Compile every source and link the shared library, then the module of torch
+    calls (where that cannot be built the library is there all the same);
+    returns the library's path."""
     os.makedirs(OUT_DIR, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as ex:
         torch_obj = ex.submit(_compile_torch_ops)
