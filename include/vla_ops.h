@@ -148,9 +148,10 @@ vla_status vla_op_qk_norm_rope(const vla_heads *q, const vla_heads *k, vla_dtype
  * vla_op_kv4_bytes bytes of device memory (16-byte aligned), sequence by
  * sequence, head by head, opaque within.  Every 32 dims of a key or value row
  * share m = min and s = (max - min) * (1 / 15), an fp32 product rounded to
- * bf16; a value x is held as c = (x - m) / s rounded to the nearest (ties to
- * even) and at most 15, and stands for m + s c.  Groups whose range is below 2^-99 are held as m;
- * groups with a value that is not finite read back as NaN.
+ * bf16; a value x is held as c = (x - m) / s, the difference rounded to fp32,
+ * the quotient to the nearest whole number (ties to even), at most 15, and
+ * stands for m + s c.  Groups whose range is below 2^-99 are held as m; groups
+ * with a value that is not finite read back as NaN.
  * store puts rows k, v[B][L][Hkv][dh] (bf16) at positions start[b] + t, t <
  * count[b] (device int32; NULL: start 0, count L; count is cut to [0, L]);
  * load takes them out into k, v.  Positions outside [0, L_cap) are left out,

@@ -90,11 +90,14 @@ struct Group4 {
   uint32_t params;  // of the group
 };
 // The codes of 8 values whose group spans [lo, lo + d], with step s and its
-// approximate inverse.  The quotient is corrected once by its remainder: x -
-// lo and s have at most 17 and 8 significant bits, so a quotient on a border
-// between two codes is exactly representable and comes out exact; s lies within
-// 2^-9 of d / 15, so none rounds to more than 15.  Halves of a word are summed
-// up in fp32, 16 bits each.
+// approximate inverse.  t = x - lo is rounded to fp32, as in plain fp32 code (lo
+// = -2.5, s = 1, x = 2^-30: 2.5, code 2); from there on a code is t / s rounded once.
+// The quotient is corrected once by its remainder.  Where t / s is a border k + 1/2
+// between two codes it comes out exact.  Elsewhere t is at least one fp32 step from
+// (k + 1/2) s, which has 13 bits, so t / s is off the border by 2^-24 of itself and
+// more (s, of 8 bits, keeps t's mantissa from 2 by 2^-7), and rounding it to fp32
+// takes less.  s lies within 2^-9 of d / 15, so none rounds to more than 15.
+// Halves of a word are summed up in fp32, 16 bits each.
 __device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float lo, float s, float inv) {
   float half[2] = {0.f, 0.f};
 #pragma unroll
