@@ -63,4 +63,26 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
+// ---- 4-bit codes as MFMA operands (w4.hip, kv4.hip)
+__host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
+
+// 8 codes of a word as bf16 numbers 16 + c: rotated left by 3, a word's nibbles i
+// and 4 + i lie at the top mantissa bits (3-6) of a pair of 16.0, 4 i bits to the right.
+// The constants sit in registers of their own, hidden from the compiler: and-or
+// takes no literals, and two instructions in its place cost a third of the
+// unpacking.
+struct UnpackCodes {
+  uint32_t bias = 0x41804180u, mask = 0x00780078u;
+  __device__ __forceinline__ UnpackCodes() { asm("" : "+s"(bias), "+v"(mask)); }
+  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
+    const u32x4 v = {(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
+                     (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias,
+                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
+    return __builtin_bit_cast(bf16x8, v);
+  }
+};
+__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
 static constexpr inline int cdiv(int a, int b) { return (a + b - 1) / b; }

@@ -45,21 +45,8 @@ constexpr float RAISE = 8.f;  // log2 by which scores may rise before the maximu
 constexpr int MOST = 15, PLACE = 7;
 constexpr float MID = 7.5f;  // of the codes
 constexpr int KROT = 3, VROT = 6;
-__host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
 
-// Words of codes to operands.  The constants sit in registers of their own,
-// hidden from the compiler: and-or takes no literals, and two instructions in its
-// place cost a third of the loop's unpacking.
-struct UnpackKeys {
-  uint32_t bias = 0x41804180u, mask = 0x00780078u;
-  __device__ __forceinline__ UnpackKeys() { asm("" : "+s"(bias), "+v"(mask)); }
-  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
-    const u32x4 v = {(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
-                     (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias,
-                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
-    return __builtin_bit_cast(bf16x8, v);
-  }
-};
+// 8 codes of a word of value codes, constants in registers as in UnpackCodes:
 // pairs 0 and 2 are 16 + c, pairs 1 and 3 256 + c
 struct UnpackValues {
   uint32_t bias16 = 0x4c004c00u, mask16 = 0x03c003c0u, bias256 = 0x5c005c00u, mask256 = 0x003c003cu;
@@ -75,10 +62,7 @@ struct UnpackValues {
 };
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
+using ::mfma;  // of bf16, beside the one of fp16
 __device__ __forceinline__ f32x4 mfma(const f16x8& a, const f16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
@@ -491,7 +475,7 @@ __global__ __launch_bounds__(W * 64, R == 1 ? 3 : 2) void kv4_attention_kernel(K
   const uint8_t* const own = (const uint8_t*)a.cache + (size_t)bh * bytes;
   uint32_t* pw = lds[wave];
   const int prow = (c16 >> 2) * R + min(c16 & 3, R - 1);
-  const UnpackKeys uk;
+  const UnpackCodes uk;
   const UnpackValues uv;
   // what the value operands of this lane's keys have above their codes, and MID, in 16ths
   const _Float16 over = (_Float16)((c16 & 1 ? 256 + MID : 16 + MID) / 16);

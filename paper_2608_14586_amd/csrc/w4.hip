@@ -42,25 +42,6 @@ namespace {
 __host__ __device__ inline size_t code_bytes(int N, int K) { return (size_t)cdiv(N, 16) * cdiv(K, 128) * 1024; }
 
 constexpr int ROT = 3;
-__host__ __device__ constexpr uint32_t rotl(uint32_t w, int n) { return w << n | w >> (32 - n); }
-
-// 8 codes of a word as bf16 numbers 16 + c.  The two constants sit in registers
-// of their own, hidden from the compiler: and-or takes no literals, and two
-// instructions in its place cost a third of the loop's unpacking.
-struct Unpack {
-  uint32_t bias = 0x41804180u, mask = 0x00780078u;
-  __device__ __forceinline__ Unpack() { asm("" : "+s"(bias), "+v"(mask)); }
-  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
-    const u32x4 v = {(w & mask) | bias, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | bias,
-                     (__builtin_amdgcn_alignbit(w, w, 8) & mask) | bias,
-                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | bias};
-    return __builtin_bit_cast(bf16x8, v);
-  }
-};
-
-__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
 
 struct W4Args {
   const bf16_t* x;
@@ -104,7 +85,7 @@ __global__ __launch_bounds__(W * 64) void w4_kernel(W4Args a) {
   const int mrows = min(a.M - m0, 16);
   const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(
       (void*)(a.x + (size_t)m0 * a.ldx), (short)0, (int)(((size_t)(mrows - 1) * a.ldx + a.K) * 2), 0x00020000);
-  const Unpack unpack;
+  const UnpackCodes unpack;
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
   float y[NT][R];
 #pragma unroll
