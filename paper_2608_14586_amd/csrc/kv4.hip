@@ -815,16 +815,17 @@ struct Plan {
 };
 // Queries a tile (4 R), waves a workgroup and blocks a wave, by the estimated
 // time of each choice, in hundredths of a microsecond: a wave alone on its SIMD
-// takes 80 a block, a SIMD 37 a block and 32 more a wave, 13% and 50% more with
+// takes 75 a block, a SIMD 35 a block and 37 more a wave, 5% and 46% more with
 // R = 2 and 4 (instruction latency and the LDS round trip weigh more than
-// instructions; dh hardly shows), and a launch 46 more; one CU takes the
-// workgroups past 256; joining splits costs 360, and 44 more past every 16
-// splits.  Over 86 calls timed at every choice (1 to 128 sequences, 1 to 131072
-// tokens, 1 to 256 queries a KV head, windows), up to 100 each, what this takes is
-// 0.5% slower than the fastest on average and 7% at most.  Smaller tiles than
-// the queries need unpack the cache again for each, but where whole ones leave
-// CUs idle they are faster: 16 sequences of 12 queries over 8 heads and a window
-// of 1024, one tile 13.5 us, two 10.1.
+// instructions; dh hardly shows), and a launch 66 and 209 more (a wave's first
+// block sets a range for each query and group); one CU takes the workgroups past
+// 256; joining splits costs 231, and 22 more past every 16 splits.  Over 86 calls
+// timed at every choice (1 to 128 sequences, 1 to 131072 tokens, 1 to 256 queries a
+// KV head, windows), up to 100 each, what this takes is 0.9% slower than the
+// fastest on average and 9% at most.  Smaller tiles than the queries need unpack
+// the cache again for each, but where whole ones leave CUs idle they are faster:
+// 16 sequences of 12 queries over 8 heads and a window of 1024, one tile 15.5 us,
+// two 10.6.
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv);
   Plan p{};
@@ -833,13 +834,13 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
   for (int R = 1; R == 1 || (R <= 4 && 2 * R < rows); R *= 2) {
     const int tiles = (rows + 4 * R - 1) / (4 * R);
     const int64_t bt = (int64_t)B * Hkv * tiles;
-    const int64_t slower = R == 1 ? 100 : R == 2 ? 113 : 150, more = R == 1 ? 0 : 46;
+    const int64_t slower = R == 1 ? 100 : R == 2 ? 105 : 146, more = R == 1 ? 0 : R == 2 ? 66 : 209;
     for (int W = 4; W <= 8; W += 4) {
       const unsigned most = (blocks + W - 1) / W;
       auto consider = [&](unsigned per) {
         const unsigned ns = (blocks + per * W - 1) / (per * W);
-        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 80ll * per, simd = a_simd * (37 * per + 32);
-        const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 360 + 44 * ((ns - 1) / 16) : 0);
+        const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 75ll * per, simd = a_simd * (35 * per + 37);
+        const int64_t cost = (wave > simd ? wave : simd) * slower / 100 + more + (ns > 1 ? 231 + 22 * ((ns - 1) / 16) : 0);
         if (cost < best && ns <= limit && tiles <= 65535)
           best = cost, p = Plan{R, W, tiles, (int)(per * W), (int)ns};
         return wave * slower / 100 + more < best;  // else longer runs of blocks cost no less

@@ -77,26 +77,36 @@ def _stored(k, v, lens, L_cap):
 @pytest.mark.parametrize("power", [10, 20, 24, 28, 34, 60, 110])
 @pytest.mark.parametrize("dh,n,window,sinks", [(64, 32, 0, 0), (128, 45, 0, 0), (64, 300, 0, 0), (128, 700, 90, 3)])
 def test_values_that_a_query_does_not_see(power, dh, n, window, sinks):
+    _unseen(power, 1, 3, 2, 2, dh, n, window, sinks)  # a head's three queries share a tile
+
+
+@pytest.mark.parametrize("power", [20, 34])
+@pytest.mark.parametrize("B,Lq,H,Hkv,dh,n", [(13, 11, 7, 1, 64, 420), (13, 11, 7, 1, 128, 3000), (3, 19, 36, 3, 64, 900)])
+def test_values_that_a_query_of_a_large_tile_does_not_see(power, B, Lq, H, Hkv, dh, n):
+    _unseen(power, B, Lq, H, Hkv, dh, n, 0, 0)
+
+
+def _unseen(power, B, Lq, H, Hkv, dh, n, window, sinks):
     """The last of several tokens, and with a window those between the first
     tokens and the last query's window, have values 2^power times the others'.  Queries
     that do not see them: the result without them, to the last bit, and right."""
-    B, Lq, H, Hkv = 1, 3, 2, 2  # a head's three queries share a tile
     k, v = _kv(("unseen", dh, n), B, n, Hkv, dh)
     q = ref.normal(("unseenq", dh, n), (B, Lq, H, dh))
     big = v.copy()
-    big[0, -1] = ref.bf16(big[0, -1] * 2.0 ** power)  # the last query alone sees it
+    big[:, -1] = ref.bf16(big[:, -1] * 2.0 ** power)  # the last query alone sees it
     if window:  # the first query alone sees this one
-        big[0, n - Lq - window + 1] = ref.bf16(big[0, n - Lq - window + 1] * 2.0 ** power)
+        big[:, n - Lq - window + 1] = ref.bf16(big[:, n - Lq - window + 1] * 2.0 ** power)
     cap = (n + 31) // 32 * 32
-    a = _attend(ref.to_dev(q), _stored(k, v, [n], cap), cap, Hkv, [n], n, window, sinks)
-    b = _attend(ref.to_dev(q), _stored(k, big, [n], cap), cap, Hkv, [n], n, window, sinks)
-    free = slice(1, 2) if window else slice(0, 2)
-    assert np.array_equal(a[0, free], b[0, free])
-    _check(b, q, k, big, [n], window, sinks)
+    a = _attend(ref.to_dev(q), _stored(k, v, [n] * B, cap), cap, Hkv, [n] * B, n, window, sinks)
+    b = _attend(ref.to_dev(q), _stored(k, big, [n] * B, cap), cap, Hkv, [n] * B, n, window, sinks)
+    free = slice(1 if window else 0, Lq - 1)
+    assert np.array_equal(a[:, free], b[:, free])
+    _check(b, q, k, big, [n] * B, window, sinks)
 
 
 @pytest.mark.parametrize("power", [10, 20, 24, 28, 34, 50])
-@pytest.mark.parametrize("dh,H,Hkv,Lq,n", [(64, 2, 2, 1, 32), (128, 4, 1, 1, 1024), (64, 14, 2, 1, 500), (64, 7, 1, 11, 130)])
+@pytest.mark.parametrize("dh,H,Hkv,Lq,n", [(64, 2, 2, 1, 32), (128, 4, 1, 1, 1024), (64, 14, 2, 1, 500), (64, 7, 1, 11, 130),
+                                           (64, 7, 1, 11, 420), (128, 7, 1, 11, 3000)])
 def test_values_without_weight(power, dh, H, Hkv, Lq, n):
     """One early token that every query sees has a score about 60 below the others
     and values 2^power times theirs, less than its weight of 2^-85 takes away."""
@@ -130,17 +140,18 @@ def test_values_and_scores_that_run_apart(falling, dh, n):
     _check(got, q, k, v, [n])
 
 
-def test_a_query_beside_one_that_is_not_finite():
+@pytest.mark.parametrize("B,Lq,H,Hkv,dh,n", [(13, 11, 7, 1, 64, 129), (13, 11, 7, 1, 64, 420), (3, 19, 36, 3, 128, 900)])
+def test_a_query_beside_one_that_is_not_finite(B, Lq, H, Hkv, dh, n):
     """Every other query's result is the same, to the last bit."""
-    B, Lq, H, Hkv, dh, n = 13, 11, 7, 1, 64, 129
     k, v = _kv(("besidenan",), B, n, Hkv, dh)
-    cache = _stored(k, v, [n] * B, 160)
+    cap = (n + 31) // 32 * 32
+    cache = _stored(k, v, [n] * B, cap)
     q = ref.normal(("besidenanq",), (B, Lq, H, dh))
-    want = _attend(ref.to_dev(q), cache, 160, Hkv, [n] * B, n)
+    want = _attend(ref.to_dev(q), cache, cap, Hkv, [n] * B, n)
     for bad in (np.nan, np.inf, 1e30):
         x = q.copy()
         x[:, 4, 3, 5] = ref.bf16(bad)
-        got = _attend(ref.to_dev(x), cache, 160, Hkv, [n] * B, n)
+        got = _attend(ref.to_dev(x), cache, cap, Hkv, [n] * B, n)
         assert np.isfinite(want).all() and (bad == 1e30 or np.isnan(got[:, 4, 3]).all())
         got[:, 4, 3] = want[:, 4, 3]
         assert np.array_equal(got, want)
@@ -215,21 +226,30 @@ def test_rounding_of_the_weights(Lq, n, dh):
     assert (np.abs(got[..., 1:]) <= (1 + 2.0 ** -8) * (2.0 ** -11 * 7.5 + 2.0 ** -10)).all()
 
 
-# Sizes at which the call takes 4, 8 and 16 queries a tile, 4 and 8 waves, one split,
-# several, and more than the 64 that are joined at a time; no number of query
-# rows is a multiple of the tile's.  The last column: blocks a wave takes at most.
+# Sizes at which the call takes 4, 8 and 16 queries a tile, each with 4 and 8 waves,
+# one split, several, and more than the 64 that are joined at a time; no number of
+# query rows is a multiple of the tile's.  The last column: blocks a wave takes at most.
 SPLITS = [
     (1, 1, 1, 1, 33, 1), (1, 1, 1, 1, 1500, 1), (1, 1, 1, 1, 129, 1), (1, 1, 1, 1, 9000, 1), (1, 1, 1, 1, 40000, 2),
-    (13, 11, 7, 1, 33, 1), (1, 19, 5, 1, 1500, 1), (13, 11, 7, 1, 129, 1), (1, 19, 5, 1, 3000 + 17, 2), (1, 19, 1, 1, 80000, 4),
-    (3, 19, 36, 3, 33, 1), (1, 11, 12, 1, 2000, 1), (3, 19, 36, 3, 129, 1), (1, 11, 12, 1, 4000, 1), (1, 11, 3, 1, 80000, 4),
-    (4, 8, 32, 4, 1100, 4),
+    (1, 11, 3, 1, 4000, 2), (3, 19, 36, 3, 33, 1), (1, 11, 12, 1, 2000, 2), (1, 19, 5, 1, 1500, 1), (1, 19, 5, 1, 3017, 2),
+    (13, 11, 21, 3, 33, 1), (2, 19, 9, 3, 2000, 2), (13, 11, 7, 1, 420, 2), (1, 11, 12, 1, 6000, 2), (1, 19, 1, 1, 40000, 2),
+    (8, 19, 96, 8, 33, 1), (13, 11, 7, 1, 3000, 4), (3, 19, 36, 3, 900, 4), (2, 19, 9, 3, 9000, 4), (1, 19, 1, 1, 80000, 4),
+    (4, 8, 32, 4, 1100, 5), (13, 11, 7, 1, 129, 2), (3, 19, 36, 3, 129, 2), (1, 11, 12, 1, 4000, 3),
 ]
+LONGEST = (1, 5, 5, 1, 200000, 7)  # 16 queries a tile and more than 64 splits
 
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("case", range(len(SPLITS)))
 def test_every_way_to_split(case, dh):
-    B, Lq, H, Hkv, n, steps = SPLITS[case]
+    _split(case, dh, *SPLITS[case])
+
+
+def test_many_splits_of_large_tiles():
+    _split("longest", 64, *LONGEST)
+
+
+def _split(case, dh, B, Lq, H, Hkv, n, steps):
     lens = [n - (b * n) // (2 * B) for b in range(B)]
     k, v = _kv(("splits", case, dh), B, n, Hkv, dh)
     # no two parts of the sequence have the same mean: none can be left out or taken twice
