@@ -171,6 +171,8 @@ vla_status vla_op_kv4_load(const void *cache, const int32_t *start, const int32_
  * Lq + i and o[b][i][h] (bf16) = softmax(q k_j / sqrt(dh)) v_j over the keys
  * j <= p of KV head h / (H / Hkv) -- with window > 0 over those with j > p -
  * window or j < sinks (a sliding window, and first tokens that stay visible).
+ * Made for a decode step's few tokens: every 16 queries of a KV head or less
+ * read the cache once more.
  * A query that sees no key (p < 0) gives zeros.  Cached rows that no query
  * sees may hold anything.  max_len: no sequence is longer (lens above it, or
  * below 0, are cut), max_len <= L_cap; it decides how the work is split, so

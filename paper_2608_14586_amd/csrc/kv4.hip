@@ -200,7 +200,8 @@ __device__ __forceinline__ Span span_of(const Kv4Rows& a, int wg) {
 // values take as long as the memory does, so there are workgroups enough for
 // two rounds, whose loads and arithmetic overlap.  The value codes cross LDS
 // to the threads that hold 8 dims of 8 tokens and transpose them.  2048 tokens of
-// 32 heads, dh = 128 (44 MB): 12.1 us, 3.6 TB/s; with the arithmetic left out 9.7.
+// 32 heads, dh = 128 (44 MB): 12.2 us where they lie in the 256 MB cache, 3.6 TB/s
+// (9.7 with the arithmetic left out), from memory 14.4.
 template <int DH>
 __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows a) {
   constexpr int LPR = DH / 8, RPP = 256 / LPR, P = BLK / RPP, NG = DH / 32, ND = DH / 16;  // lanes a row, rows a pass
@@ -261,7 +262,8 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows a) {
 }
 
 // The inverse: 4 DH / 8 threads transpose the block's value codes into LDS,
-// word j of every token as the keys have it.  8.6 us for the same 44 MB, 5.1 TB/s.
+// word j of every token as the keys have it.  8.4 us for the same 44 MB, 5.2 TB/s, and
+// 14.0 where the cache is read from memory and the rows go there.
 template <int DH>
 __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
   constexpr int LPR = DH / 8, RPP = 256 / LPR, P = BLK / RPP, NG = DH / 32, ND = DH / 16;
@@ -339,17 +341,19 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // P crosses from score lanes (one key each) to operand lanes (8 keys of one
 // query) through LDS, as 32-bit pairs of the keys t and t + 16: that pairing
 // is why the value codes of those tokens share a word's halves.
+// More than 16 queries a KV head unpack the cache once for each 16 and less: 2048
+// tokens, 32 heads over 8, one token's queries 6.2 us, 16 tokens' 12, 256 tokens' 34.
 // Work is split over the keys: waves of a workgroup take every W-th block of
 // 32 keys, workgroups contiguous runs of them, joined in LDS and by
 // kv4_combine_kernel.
-// With R = 1 and dh = 128 a block is about 210 vector instructions and 16 MFMAs
+// With R = 1 and dh = 128 a block is about 220 vector instructions and 16 MFMAs
 // a wave against 5120 bytes.  A wave alone on its SIMD takes 0.8 us a block that
 // lies in cache and 1.2 from memory, two side by side 1.1 and 1.9: the memory
-// comes first.  156 registers leave three waves a SIMD; two took a third longer
+// comes first.  159 registers leave three waves a SIMD; two took a third longer
 // over long caches, and four spill.  Eight sequences of up to 32768 tokens (32
 // heads, 8 KV heads, 189 MB) take 42.7 us, 4.4 TB/s, joining and ragged ends
-// included; one of 2049 tokens (32 KV heads) 7.9 us, of which two launches are
-// 4.6.
+// included; one of 2049 tokens (32 KV heads) 7.5 us where it lies in
+// the 256 MB cache and 8.8 from memory, of which two launches are 4.6.
 // The loads of the next block go out in two parts, each into the registers that
 // the part of this block before it has used up, unconditionally and below a
 // scheduling barrier: with branches around them, or with a use of the old values
@@ -803,7 +807,7 @@ unsigned blocks_of(int Lq, int max_len, int window, int sinks) {
 // which the last round of 256 costs 3% at most, of four blocks or more.  It never
 // falls with the length, which a plan's own number does, so scratch for the longest call
 // serves each shorter one; of 100000 drawn calls (1 to 128 sequences, 1 to 140000 tokens)
-// 0.9% would take more splits and lose 0.02% of their estimated time on average.
+// 0.7% would take more splits, and lose 2% of their estimated time on average.
 unsigned most_splits(int B, int Lq, int H, int Hkv, unsigned blocks) {
   const int rows = Lq * (H / Hkv), tile = rows > 8 ? 16 : rows > 4 ? 8 : 4;
   const int64_t wgs = (int64_t)B * Hkv * ((rows + tile - 1) / tile), n = (8191 + wgs) / wgs;

@@ -18,9 +18,15 @@
 // eight times that).
 //
 // That leaves 7 instructions and an MFMA for the 512 weights of a word a lane, so
-// the stream of weights is the bound where it is long: 26 MB (N = 12288, K =
-// 4096, one row) take 6.5 us, 2.3 of them a launch's own; 48 MB (gated, 2 x 11008,
-// K = 4096, four rows) 10 us; 29 MB with 13 rows (N = 4096, K = 11008) 8.6 us.
+// the stream of weights is the bound where it is long, us from the 256 MB cache
+// (three calls' weights in turn) and from memory (1.3 GB in turn, as the layers of
+// a decode step read them; 2.3 are a launch's own):
+//   26 MB, N = 12288, K = 4096, one row:  6.4, 7.2
+//   48 MB, gated, 2 x 11008, K = 4096, four rows:  10.0, 12.0
+//   29 MB, N = 4096, K = 11008, 13 rows:  8.7, 12.3
+// The last has 256 workgroups of six blocks of k in a row for each wave, and a
+// block from memory takes longer.  More than 16 rows read the weights once per 16:
+// N = 12288, K = 4096, 64 rows 16 us, 256 rows 52 (the bf16 product of 256 rows: 31).
 //
 // Rows of x sit in the accumulator rows that one register of the MFMA result
 // covers: with M <= 4 in rows 0, 4, 8, 12, so a lane holds one useful value
@@ -287,7 +293,9 @@ Shape shape_of(int M, int N, int K, bool swiglu) {
   return best;
 }
 
-// one thread per word of the packed weights
+// One thread per word of the packed weights, whose 8 codes are bytes of one row;
+// neighbours in a wave take rows K apart.  Once a matrix, at load: N = 12288, K =
+// 4096 (50 MB of codes, 27 packed) 87 us, 0.9 TB/s.
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict__ codes,
                                                       const bf16_t* __restrict__ scales,
                                                       const bf16_t* __restrict__ zeros, uint32_t* __restrict__ wp, int N,

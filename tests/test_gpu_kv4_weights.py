@@ -226,6 +226,22 @@ def test_rounding_of_the_weights(Lq, n, dh):
     assert (np.abs(got[..., 1:]) <= (1 + 2.0 ** -8) * (2.0 ** -11 * 7.5 + 2.0 ** -10)).all()
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("bits", [16, 19, 22, 25, 28, 31])
+def test_many_small_weights(bits, dh):
+    """One key, and 4000 of weights 2^-bits of its: their p s are subnormal as fp16, or
+    nothing, and what the codes' offset of up to 256 makes of them is taken off to
+    the last bit.  The one key's values are 0, which leaves nothing else to see."""
+    B, H, Hkv, n = 1, 8, 1, 4000
+    k, v = _kv(("small", dh), B, n, Hkv, dh)
+    q = ref.normal(("smallq", dh), (B, 1, H, dh), 0.02)
+    k[..., 0], q[..., 0] = 0.0, 8.0
+    k[:, 0, :, 0] = ref.bf16(bits * np.log(2) * np.sqrt(dh) / 8.0)
+    v[:, 0] = np.where(np.arange(dh) % 32 == 0, -15.0, 0.0)
+    got = _attend(ref.to_dev(q), _stored(k, v, [n], n), n, Hkv, [n], n)
+    _check(got, q, k, v, [n], steps=17)
+
+
 # Sizes at which the call takes 4, 8 and 16 queries a tile, each with 4 and 8 waves,
 # one split, several, and more than the 64 that are joined at a time; no number of
 # query rows is a multiple of the tile's.  The last column: blocks a wave takes at most.
