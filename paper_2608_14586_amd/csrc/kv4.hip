@@ -331,11 +331,11 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 //    2^6 and 2^15.  So a key weighs in a query's unit by what it adds to that query, and
 //    one that the query does not see, or gives no weight, moves nothing, however
 //    large its values.  The second sum is of the rounded P', so that rounding costs
-//    2^-11 of at most 7.5 s_g P a key, a quarter of a bf16 result's own rounding of
-//    15 s_g P, and less than 2^-31 of the largest P' where P' is subnormal.  (Without the
-//    7.5, the middle of the codes, it would be twice that, for 8 of 215 instructions; in
-//    bf16 eight times; hi and lo bf16 parts cost 12 instructions a row and group
-//    against 6.)
+//    2^-11 of at most 7.5 s_g P a key, a sixteenth of what a bf16 result's rounding
+//    takes of 15 s_g P, and less than 2^-31 of the largest P' where P' is subnormal.
+//    (Without the 7.5, the middle of the codes, it would be twice that, for 8 of 220
+//    instructions; in bf16 eight times; hi and lo bf16 parts cost 12 instructions
+//    a row and group against 6.)
 // The 4 R queries of a tile sit in the MFMA rows 4 i + r, r < R, so with up to
 // four of them a lane holds one useful score a key and not four (R = 1).
 // P crosses from score lanes (one key each) to operand lanes (8 keys of one
@@ -352,8 +352,8 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows a) {
 // comes first.  159 registers leave three waves a SIMD; two took a third longer
 // over long caches, and four spill.  Eight sequences of up to 32768 tokens (32
 // heads, 8 KV heads, 189 MB) take 42.7 us, 4.4 TB/s, joining and ragged ends
-// included; one of 2049 tokens (32 KV heads) 7.5 us where it lies in
-// the 256 MB cache and 8.8 from memory, of which two launches are 4.6.
+// included; one of 2049 tokens (32 KV heads) 7.5 us where it lies in the 256 MB
+// cache and 8.8 from memory, of which two launches are 4.6.
 // The loads of the next block go out in two parts, each into the registers that
 // the part of this block before it has used up, unconditionally and below a
 // scheduling barrier: with branches around them, or with a use of the old values
