@@ -72,7 +72,7 @@ def draw(rng):
     if op == "gemm":
         out = rng.choice(["bf16", "f32", "add", "swiglu"])
         K = 16 * _log_int(rng, 16, 688)
-        N = 32 * _log_int(rng, 8, 688) if out == "swiglu" else _log_int(rng, 256, 12288)
+        N = 64 * _log_int(rng, 4, 344) if out == "swiglu" else _log_int(rng, 256, 12288)
         M = rng.choice([rng.randint(1, 16), _log_int(rng, 17, max(18, min(4096, 180_000_000_000 // (N * K))))])
         return {"op": "gemm", "M": M, "N": N, "K": K, "out": out}
     H, Hkv = rng.choice(HEADS)
