@@ -187,6 +187,52 @@ vla_status vla_op_attention_kv4(const vla_heads *q, const void *cache, const int
                                 int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,
                                 void *scratch, size_t scratch_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * A block in 8 bits over prompts of different lengths, and the 8-bit KV cache
+ * that decode steps read afterwards.  Prompts lie behind one another, T rows in
+ * all.  The attention half is: vla_op_norm_i8, vla_op_gemm_i8 (QKV),
+ * vla_op_qk_norm_rope, vla_op_kv8_store, vla_op_attention_packed (whole prompts)
+ * or vla_op_attention_kv8 (a decode step's tokens), vla_op_norm_i8 without a gain,
+ * vla_op_gemm_i8 (output projection); the MLP half vla_op_norm_i8 with the
+ * residual's addition, vla_op_gemm_i8 with swiglu, vla_op_norm_i8 without a gain,
+ * vla_op_gemm_i8.  What the 4-bit section says of memory, graphs, devices and
+ * errors holds here too.
+ */
+
+/* Rows into int8 codes with a scale each.  With a gain g[d] (fp32), the RMS norm
+ * of t = x + add: row value j is close to t_j g_j / sqrt(mean(t^2) + eps) and is held
+ * as codes[j] * scales[row]; without (g NULL; eps is not used), close to t_j.
+ * x[M][d] in x_dtype; add[M][d] in add_dtype or NULL; sum[M][d] (fp32, NULL: not
+ * wanted) receives t, and may be x or add themselves (fp32, same strides).
+ * u = t g (t without a gain) and t are rounded to fp32; a code is 127 u / max|u| of
+ * the row to the nearest whole number, ties to even, the scale max|u| / 127, times the
+ * norm's factor with a gain.  A row whose max|u| is below 2^-100 is held as zeros (scale
+ * 0), one with a value that is not finite as codes of 0 with the scale NaN.
+ * Row strides in elements, no less than d where M > 1, multiples of 8; gain and
+ * rows 16-byte aligned, codes 8-byte.  d % 8 == 0, d <= 32768, eps >= 0. */
+vla_status vla_op_norm_i8(const void *x, int64_t ldx, vla_dtype x_dtype, const void *add, int64_t ldadd,
+                          vla_dtype add_dtype, float *sum, int64_t ldsum, const float *g, float eps, void *codes,
+                          int64_t ldc, float *scales, int M, int d, void *stream);
+
+/* 8-bit weights: W[n][k] = scales[n] * codes[n][k].  vla_op_w8_pack lays codes[N][K]
+ * (int8) and scales[N] (fp32) out for vla_op_gemm_i8, in Wp of
+ * vla_op_w8_packed_bytes bytes.  All DEVICE pointers, 16-byte aligned (scales: 4).
+ * K % 16 == 0, K <= 131056, N < 2^25.  vla_op_w8_packed_bytes is 0 for sizes that are refused. */
+size_t vla_op_w8_packed_bytes(int N, int K);
+vla_status vla_op_w8_pack(const void *codes, const float *scales, void *Wp, int N, int K, void *stream);
+
+/* out[M][N] = sx[m] * scales[n] * sum_k x[m][k] codes[n][k] + residual[M][N] (fp32,
+ * NULL = none), x[M][K] int8 with a scale a row, sx[M] (fp32), W the packed 8-bit
+ * weights, out in out_dtype.  The sum is exact, whatever M.
+ * swiglu: W holds N / 2 gate rows, then the N / 2 up rows, and out[M][N / 2] =
+ * silu(x Wgate^T) * (x Wup^T) + residual; N % 64 == 0.
+ * Row strides in elements, no less than a row's width where M > 1: ldx of x (a
+ * multiple of 16; x 16-byte aligned), ldo of out and of residual, which may be the
+ * same memory (fp32 out).  A scale of x that is not finite gives a row of out that is
+ * not finite, and reaches no other row. */
+vla_status vla_op_gemm_i8(const void *x, int64_t ldx, const float *sx, const void *Wp, const float *residual, void *out,
+                          int64_t ldo, vla_dtype out_dtype, int swiglu, int M, int N, int K, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

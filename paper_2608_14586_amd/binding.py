@@ -125,6 +125,11 @@ def lib():
                                 c_void_p],
             "vla_op_attention_kv4": [c_char_p, c_void_p, c_void_p, c_char_p, c_int, c_int, c_int, c_int, c_int, c_int,
                                      c_int, c_int, c_int, c_void_p, c_size_t, c_void_p],
+            "vla_op_norm_i8": [c_void_p, c_int64, c_int, c_void_p, c_int64, c_int, c_void_p, c_int64, c_void_p, c_float,
+                               c_void_p, c_int64, c_void_p, c_int, c_int, c_void_p],
+            "vla_op_w8_pack": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p],
+            "vla_op_gemm_i8": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
+                               c_int, c_int, c_void_p],
             "vla_suffix_create": [P(vla_stack_cfg), c_int, c_int, c_int, P(c_void_p)],
             "vla_suffix_load_block_weights": [c_void_p, c_int, P(vla_block_weights)],
             "vla_suffix_run": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
@@ -148,7 +153,8 @@ def lib():
             fn.restype = c_int
         L.vla_op_packed_weight_elems.argtypes = [c_int, c_int]
         L.vla_op_packed_weight_elems.restype = c_size_t
-        for name, n in (("vla_op_w4_packed_bytes", 3), ("vla_op_kv4_bytes", 4), ("vla_op_attention_kv4_scratch", 8)):
+        for name, n in (("vla_op_w4_packed_bytes", 3), ("vla_op_kv4_bytes", 4), ("vla_op_attention_kv4_scratch", 8),
+                        ("vla_op_w8_packed_bytes", 2)):
             getattr(L, name).argtypes = [c_int] * n
             getattr(L, name).restype = c_size_t
         L.vla_status_string.argtypes = [c_int]
@@ -413,7 +419,7 @@ def vla_op_gemm_tile_bf16(op, tile, A, Wp, out, bias, M, N, K, stream=None):
 
 
 # ----------------------------------------- 4-bit weights and KV cache (torch)
-# These calls take torch tensors on the GPU and read sizes and strides off
+# These calls, and the 8-bit ones behind them, take torch tensors on the GPU and read sizes and strides off
 # them (csrc/torch_ops.cpp); a tensor whose type, shape, device or size does
 # not fit raises ValueError before the library is called.  `stream`: a
 # hipStream_t (torch's `stream.cuda_stream`), None = torch's current stream, so
@@ -494,6 +500,38 @@ def vla_op_attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window=0, sinks
     """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a tensor of
     vla_op_attention_kv4_scratch(...) bytes (None where that is 0)."""
     code = (_torch_ops or _ops()).attention_kv4(q, cache, L_cap, Hkv, lens, o, max_len, window, sinks, scratch, stream)
+    if code:
+        _check(code)
+
+
+# -------------------------------------- 8-bit rows, weights and KV cache (torch)
+
+def vla_op_norm_i8(x, add, sum, g, eps, codes, scales, stream=None):
+    """x [M, d] and add (or None) float32 or bfloat16 -> codes [M, d] int8, scales
+    [M] float32; sum (or None) [M, d] float32 receives x + add.  g [d] float32: the
+    RMS norm with that gain; None: the rows themselves."""
+    code = (_torch_ops or _ops()).norm_i8(x, add, sum, g, eps, codes, scales, stream)
+    if code:
+        _check(code)
+
+
+def vla_op_w8_packed_bytes(N, K):
+    return lib().vla_op_w8_packed_bytes(N, K)
+
+
+def vla_op_w8_pack(codes, scales, Wp, stream=None):
+    """codes [N, K] int8, scales [N] float32 -> Wp, a tensor of
+    vla_op_w8_packed_bytes(N, K) bytes."""
+    code = (_torch_ops or _ops()).w8_pack(codes, scales, Wp, stream)
+    if code:
+        _check(code)
+
+
+def vla_op_gemm_i8(x, sx, Wp, residual, out, N, swiglu=False, stream=None):
+    """x [M, K] int8 with scales sx [M] float32, residual (None or float32) and out
+    [M, N or N / 2] (float32 or bfloat16), rows of any stride; residual's rows
+    and out's are equally far apart."""
+    code = (_torch_ops or _ops()).gemm_i8(x, sx, Wp, residual, out, N, swiglu, stream)
     if code:
         _check(code)
 

@@ -1,5 +1,5 @@
 """Compile the HIP kernels and the C-ABI runtime into ``libvlaprefix.so``
-(gfx950 only) with hipcc, and the binding's torch calls of the 4-bit operators
+(gfx950 only) with hipcc, and the binding's torch calls of the 4-bit and 8-bit operators
 into ``_torch_ops.so``.  Objects go to ``_build/`` next to this file."""
 from __future__ import annotations
 
@@ -24,7 +24,7 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-fPIC", "-std=c++17", "-Xclang
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result"]
 
 SOURCES = ["gemm_bf16.hip", "attention_bf16.hip", "decode_bf16.hip", "norm.hip", "fp32_path.hip", "vision.hip",
-           "static_scratch.hip", "w4.hip", "qk_norm.hip", "kv4.hip",
+           "static_scratch.hip", "w4.hip", "qk_norm.hip", "kv4.hip", "norm_i8.hip", "w8.hip",
            "runtime.cpp",
            "ops.cpp",
            "host_suffix.cpp", "host_suffix_api.cpp", "sched.cpp"]
@@ -56,7 +56,7 @@ def _compile(src: str) -> str:
 def _torch_dir() -> str:
     spec = importlib.util.find_spec("torch")
     if spec is None:
-        raise RuntimeError("_torch_ops.so, the 4-bit operators on torch tensors, needs torch's headers and libraries, "
+        raise RuntimeError("_torch_ops.so, the 4-bit and 8-bit operators on torch tensors, needs torch's headers and libraries, "
                            "and torch is not installed (libvlaprefix.so does without)")
     return list(spec.submodule_search_locations)[0]
 
@@ -71,7 +71,7 @@ def _compile_torch_ops() -> str:
     try:
         r = subprocess.run(cmd, capture_output=True, text=True)
     except FileNotFoundError:
-        raise RuntimeError("_torch_ops.so, the 4-bit operators on torch tensors, needs g++ (libvlaprefix.so does without)")
+        raise RuntimeError("_torch_ops.so, the 4-bit and 8-bit operators on torch tensors, needs g++ (libvlaprefix.so does without)")
     if r.returncode != 0:
         raise RuntimeError("g++ failed for torch_ops.cpp:\n%s\n%s" % (" ".join(cmd), r.stderr[-6000:]))
     return obj

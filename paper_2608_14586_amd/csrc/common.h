@@ -38,6 +38,13 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
+// the largest whole number of the wave
+__device__ __forceinline__ uint32_t wave_max_u(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+
 // A value of another lane by DPP: CTRL 0xB1 and 0x4E exchange lanes 1 and 2
 // apart, 0x141 and 0x140 mirror a row's halves and the row (16 lanes), so that
 // after the first n of the four every 2^n lanes have met.

@@ -221,6 +221,41 @@ size_t kv4_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len,
 // hipErrorOutOfMemory: a.part is smaller than kv4_attention_scratch
 hipError_t kv4_attention(Kv4Attn a, int dh, size_t scratch_bytes, hipStream_t s);
 
+// ------------------------------------------- 8-bit rows, weights and KV cache
+// Rows into 8-bit codes (norm_i8.hip): t = x + add (NULL: x), written to sum if
+// it is not NULL; with a gain g the RMS norm of t.  d % 8 == 0, d <= 32768.
+struct NormI8Args {
+  const void* x;
+  const void* add;
+  float* sum;
+  const float* g;
+  int8_t* codes;
+  float* scales;
+  int64_t ldx, ldadd, ldsum, ldc;
+  int d;
+  float eps;
+  bool x_f32, add_f32;
+};
+hipError_t norm_i8(const NormI8Args& a, int M, hipStream_t s);
+
+// Packed 8-bit weights (w8.hip): codes int8 [N][K], scales [N] fp32.
+// out[M][N] = sx sw (x W^T) + res; swiglu: out[M][N / 2] = silu(gate) * up +
+// res, gate and up the two halves of the rows, N % 64 == 0.  K % 16 == 0.
+struct GemmI8Args {
+  const int8_t* x;
+  const float* sx;
+  const uint8_t* wp;
+  const float* res;
+  void* out;
+  int64_t ldx, ldo;
+  int M, N, K;
+  bool f32, swiglu;
+  bool wide;  // N (swiglu: N / 2) and the rows of out and res fit four outputs at a time
+};
+size_t w8_packed_bytes(int N, int K);
+hipError_t w8_pack(const int8_t* codes, const float* scales, void* wp, int N, int K, hipStream_t s);
+hipError_t gemm_i8(const GemmI8Args& a, hipStream_t s);
+
 // Fixed device scratch of the decode step that allocates nothing
 // (static_scratch.hip): its size, and its address on `device` (resolved once
 // per device; `device` must be the current device the first time).

@@ -56,6 +56,12 @@ vla_status kv4_rows(const vla_heads* k, const vla_heads* v, const int32_t* start
   return VLA_OK;
 }
 
+vla_status w8_check(int N, int K) {
+  if (N <= 0 || K <= 0) return VLA_ERR_INVALID_ARG;
+  if (K % 16 || K > 131056 || N >= 1 << 25) return VLA_ERR_UNSUPPORTED;
+  return VLA_OK;
+}
+
 // window: one that covers max_len tokens hides none, and is taken out here
 vla_status attn_check(int B, int Lq, int H, int Hkv, int dh, int max_len, int* window, int* sinks) {
   if (B < 0 || Lq < 0 || H <= 0 || Hkv <= 0 || max_len < 0 || *window < 0 || *sinks < 0) return VLA_ERR_INVALID_ARG;
@@ -245,6 +251,57 @@ vla_status vla_op_attention_kv4(const vla_heads* q, const void* cache, const int
                        0, 0, 0, {}, {}, {}, {}, 0.f};
   const hipError_t e = vla::kv4_attention(a, dh, scratch_bytes, (hipStream_t)stream);
   return e == hipErrorOutOfMemory ? VLA_ERR_SHAPE : status_of(e);
+}
+
+// ------------------------------------------------- 8-bit rows, weights and KV cache
+
+vla_status vla_op_norm_i8(const void* x, int64_t ldx, vla_dtype x_dtype, const void* add, int64_t ldadd,
+                          vla_dtype add_dtype, float* sum, int64_t ldsum, const float* g, float eps, void* codes,
+                          int64_t ldc, float* scales, int M, int d, void* stream) {
+  if (M < 0 || d <= 0 || ldx < 0 || ldadd < 0 || ldsum < 0 || ldc < 0 || (x_dtype != VLA_BF16 && x_dtype != VLA_F32) ||
+      (add && add_dtype != VLA_BF16 && add_dtype != VLA_F32) || (g && !(eps >= 0.f)) || (M && (!x || !codes || !scales)))
+    return VLA_ERR_INVALID_ARG;
+  if (M > 1 && (ldx < d || (add && ldadd < d) || (sum && ldsum < d) || ldc < d)) return VLA_ERR_INVALID_ARG;
+  // a launch has at most 1024 threads a row, fewer than 2^32 in all
+  if (d % 8 || d > 32768 || M > 0x3fffff || ldx % 8 || ldadd % 8 || ldsum % 8 || ldc % 8 || !aligned(x, 16) ||
+      !aligned(add, 16) || !aligned(sum, 16) || !aligned(g, 16) || !aligned(codes, 8) || !aligned(scales, 4))
+    return VLA_ERR_UNSUPPORTED;
+  if (M == 0) return VLA_OK;
+  const vla::NormI8Args a{x,   add,   sum,    g, (int8_t*)codes, scales, ldx,
+                          ldadd, ldsum, ldc, d, eps, x_dtype == VLA_F32, add_dtype == VLA_F32};
+  return status_of(vla::norm_i8(a, M, (hipStream_t)stream));
+}
+
+size_t vla_op_w8_packed_bytes(int N, int K) { return w8_check(N, K) == VLA_OK ? vla::w8_packed_bytes(N, K) : 0; }
+
+vla_status vla_op_w8_pack(const void* codes, const float* scales, void* Wp, int N, int K, void* stream) {
+  if (!codes || !scales || !Wp) return VLA_ERR_INVALID_ARG;
+  const vla_status st = w8_check(N, K);
+  if (st != VLA_OK) return st;
+  if (!aligned(Wp, 16) || !aligned(codes, 16) || !aligned(scales, 4)) return VLA_ERR_UNSUPPORTED;
+  return status_of(vla::w8_pack((const int8_t*)codes, scales, Wp, N, K, (hipStream_t)stream));
+}
+
+vla_status vla_op_gemm_i8(const void* x, int64_t ldx, const float* sx, const void* Wp, const float* residual, void* out,
+                          int64_t ldo, vla_dtype out_dtype, int swiglu, int M, int N, int K, void* stream) {
+  if (M < 0 || ldx < 0 || ldo < 0 || (out_dtype != VLA_BF16 && out_dtype != VLA_F32) ||
+      (M && (!x || !sx || !Wp || !out)))
+    return VLA_ERR_INVALID_ARG;
+  const vla_status st = w8_check(N, K);
+  if (st != VLA_OK) return st;
+  const bool f32 = out_dtype == VLA_F32;
+  if (ldx % 16 || !aligned(x, 16) || !aligned(Wp, 16) || !aligned(sx, 4) || !aligned(out, f32 ? 4 : 2) ||
+      !aligned(residual, 4) || (swiglu && N % 64))
+    return VLA_ERR_UNSUPPORTED;
+  const int wide = swiglu ? N / 2 : N;
+  if (M > 1 && (ldx < K || ldo < wide)) return VLA_ERR_INVALID_ARG;
+  // 256 rows of x and of out lie within 2^31 bytes
+  if (M > 1 && (ldx > (1 << 30) / 256 || ldo > (1 << 30) / 1024)) return VLA_ERR_UNSUPPORTED;
+  if (M == 0) return VLA_OK;
+  const bool whole = wide % 4 == 0 && ldo % 4 == 0 && aligned(out, f32 ? 16 : 8) && aligned(residual, 16);
+  const vla::GemmI8Args a{(const int8_t*)x, sx, (const uint8_t*)Wp, residual, out, M > 1 ? ldx : 0, M > 1 ? ldo : 0,
+                          M, N, K, f32, swiglu != 0, whole};
+  return status_of(vla::gemm_i8(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// The 4-bit operators' Python calls: sizes and strides read off torch tensors,
+// The 4-bit and 8-bit operators' Python calls: sizes and strides read off torch tensors,
 // checked, and handed to the C ABI of include/vla_ops.h.
 //
 // A decode step's kernels take two to five microseconds.  Reading one tensor's
@@ -87,7 +87,38 @@ void four(const at::Tensor& t, const char* name) {
   if (t.dim() != 4) throw Misfit{name, "four dimensions"};
 }
 
-constexpr auto BF16 = at::kBFloat16, F32 = at::kFloat, I32 = at::kInt;
+constexpr auto BF16 = at::kBFloat16, F32 = at::kFloat, I32 = at::kInt, I8 = at::kChar;
+
+// [M, wide] of that type with dense rows, and its row stride (0 for one row)
+const at::Tensor& rows(PyObject* o, at::ScalarType type, int64_t M, int64_t wide, int device, const char* name, int64_t* ld) {
+  const at::Tensor& t = tensor_of(o, name);
+  on(t, device, name);
+  if (t.scalar_type() != type || t.dim() != 2 || t.size(0) != M || t.size(1) != wide || (t.stride(1) != 1 && wide != 1))
+    throw Misfit{name, "two dimensions of the type and sizes that the call's others give, with dense rows"};
+  *ld = M > 1 ? t.stride(0) : 0;
+  return t;
+}
+bool truth(PyObject* o, const char* name) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) {
+    PyErr_Clear();
+    throw Misfit{name, "True or False"};
+  }
+  return v != 0;
+}
+vla_dtype float_type(const at::Tensor& t, const char* name) {
+  if (t.scalar_type() == F32) return VLA_F32;
+  if (t.scalar_type() != BF16) throw Misfit{name, "float32 or bfloat16"};
+  return VLA_BF16;
+}
+float float_of(PyObject* o, const char* name) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) {
+    PyErr_Clear();
+    throw Misfit{name, "a number"};
+  }
+  return (float)v;
+}
 
 // args: codes, scales, zeros, Wp, group, stream
 vla_status w4_pack(PyObject* const* a) {
@@ -206,6 +237,66 @@ vla_status attention_kv4(PyObject* const* a) {
                               bytes ? scratch : nullptr, bytes, stream_of(a[10]));
 }
 
+// args: x, add, sum, g, eps, codes, scales, stream
+vla_status norm_i8(PyObject* const* a) {
+  const at::Tensor& x = tensor_of(a[0], "x");
+  const int dev = device_of(x, "x");
+  if (x.dim() != 2) throw Misfit{"x", "two dimensions"};
+  const int M = dim(x, 0, "x"), d = dim(x, 1, "x");
+  const vla_dtype xt = float_type(x, "x");
+  int64_t ldx, ldadd = 0, ldsum = 0, ldc;
+  rows(a[0], x.scalar_type(), M, d, dev, "x", &ldx);
+  vla_dtype at = VLA_BF16;
+  void *add = nullptr, *sum = nullptr;
+  if (a[1] != Py_None) {
+    at = float_type(tensor_of(a[1], "add"), "add");
+    add = rows(a[1], at == VLA_F32 ? F32 : BF16, M, d, dev, "add", &ldadd).data_ptr();
+  }
+  if (a[2] != Py_None) sum = rows(a[2], F32, M, d, dev, "sum", &ldsum).data_ptr();
+  const int64_t gs[1] = {d}, ms[1] = {M};
+  void* codes = rows(a[5], I8, M, d, dev, "codes", &ldc).data_ptr();
+  if (a[6] == Py_None) throw Misfit{"scales", "float32 [M]"};
+  return vla_op_norm_i8(x.data_ptr(), ldx, xt, add, ldadd, at, (float*)sum, ldsum, (float*)dense(a[3], F32, gs, dev, "g"),
+                        float_of(a[4], "eps"), codes, ldc, (float*)dense(a[6], F32, ms, dev, "scales"), M, d,
+                        stream_of(a[7]));
+}
+
+// args: codes, scales, Wp, stream
+vla_status w8_pack(PyObject* const* a) {
+  const at::Tensor& codes = tensor_of(a[0], "codes");
+  const int dev = device_of(codes, "codes");
+  if (codes.dim() != 2 || codes.scalar_type() != I8 || !codes.is_contiguous())
+    throw Misfit{"codes", "contiguous int8 [N, K]"};
+  const int N = dim(codes, 0, "codes"), K = dim(codes, 1, "codes");
+  const int64_t ns[1] = {N};
+  if (a[1] == Py_None) throw Misfit{"scales", "float32 [N]"};
+  return vla_op_w8_pack(codes.data_ptr(), (float*)dense(a[1], F32, ns, dev, "scales"),
+                        memory(a[2], vla_op_w8_packed_bytes(N, K), dev, "Wp"), N, K, stream_of(a[3]));
+}
+
+// args: x, sx, Wp, residual, out, N, swiglu, stream
+vla_status gemm_i8(PyObject* const* a) {
+  const at::Tensor &x = tensor_of(a[0], "x"), &out = tensor_of(a[4], "out");
+  const int dev = device_of(x, "x"), N = int_of(a[5], "N");
+  const bool swiglu = truth(a[6], "swiglu");
+  if (x.dim() != 2) throw Misfit{"x", "int8 [M, K]"};
+  const int M = dim(x, 0, "x"), K = dim(x, 1, "x");
+  const vla_dtype ot = float_type(out, "out");
+  const int64_t wide = swiglu ? N / 2 : N, ms[1] = {M};
+  int64_t ldx, ldo, ldr;
+  rows(a[0], I8, M, K, dev, "x", &ldx);
+  rows(a[4], out.scalar_type(), M, wide, dev, "out", &ldo);
+  const float* res = nullptr;
+  if (a[3] != Py_None) {
+    res = (const float*)rows(a[3], F32, M, wide, dev, "residual", &ldr).data_ptr();
+    if (ldr != ldo) throw Misfit{"residual", "out's row stride"};
+  }
+  if (a[1] == Py_None) throw Misfit{"sx", "float32 [M]"};
+  return vla_op_gemm_i8(x.data_ptr(), ldx, (float*)dense(a[1], F32, ms, dev, "sx"),
+                        memory(a[2], vla_op_w8_packed_bytes(N, K), dev, "Wp"), res, out.data_ptr(), ldo, ot, swiglu, M, N,
+                        K, stream_of(a[7]));
+}
+
 // no exception leaves a call: a misfit becomes ValueError, anything else RuntimeError
 template <vla_status (*F)(PyObject* const*), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -236,6 +327,9 @@ PyMethodDef methods[] = {method<w4_pack, 6>("w4_pack"),
                          method<kv4_store, 7>("kv4_store"),
                          method<kv4_load, 7>("kv4_load"),
                          method<attention_kv4, 11>("attention_kv4"),
+                         method<norm_i8, 8>("norm_i8"),
+                         method<w8_pack, 4>("w8_pack"),
+                         method<gemm_i8, 8>("gemm_i8"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
