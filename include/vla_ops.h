@@ -233,6 +233,38 @@ vla_status vla_op_w8_pack(const void *codes, const float *scales, void *Wp, int 
 vla_status vla_op_gemm_i8(const void *x, int64_t ldx, const float *sx, const void *Wp, const float *residual, void *out,
                           int64_t ldo, vla_dtype out_dtype, int swiglu, int M, int N, int K, void *stream);
 
+/* A KV cache of 8 bits a value for B sequences of up to L_cap tokens:
+ * vla_op_kv8_bytes bytes of device memory (16-byte aligned), opaque within.  32
+ * positions of a head (from a multiple of 32 on) are a block; the block's keys share a
+ * scale, and its values one.  A value is held as c 2^e: c a float of 8 bits (4
+ * exponent, 3 mantissa: 448 at most, steps of 2^-9 at least), e the block's exponent.
+ * store puts rows k, v[B][L][Hkv][dh] (bf16) at positions start[b] + t, t < count[b]
+ * (device int32; NULL: start 0, count L; count is cut to [0, L]).  A block whose first
+ * position is among them begins anew: e becomes the least (>= -118) for which every
+ * |x| that is stored is at most 448 2^e, and what the block held is gone.  Otherwise e
+ * grows as far as the new rows ask, and where it does the block's other codes are
+ * rounded to it; so the rows ahead of the stored ones in their block must have been
+ * stored before.  Codes are rounded to the nearest, ties to even; a value that is not
+ * finite is held as NaN and does not move e.
+ * load takes rows out into k, v, 2^e c rounded to bf16 (exact).  Positions outside [0, L_cap) are
+ * left out; other blocks of the cache (store) and rows of k, v (load) stay as they were.
+ * A call may touch one sequence's slot once; calls on one cache must be ordered
+ * (one stream).  L_cap % 32 == 0, L_cap <= 2^24, dh in {64, 128}.
+ * vla_op_kv8_bytes is 0 for sizes that are refused. */
+size_t vla_op_kv8_bytes(int B, int Hkv, int L_cap, int dh);
+vla_status vla_op_kv8_store(const vla_heads *k, const vla_heads *v, const int32_t *start, const int32_t *count,
+                            void *cache, int B, int L, int Hkv, int L_cap, int dh, void *stream);
+vla_status vla_op_kv8_load(const void *cache, const int32_t *start, const int32_t *count, const vla_heads *k,
+                           const vla_heads *v, int B, int L, int Hkv, int L_cap, int dh, void *stream);
+
+/* vla_op_attention_kv4's attention over the 8-bit cache: the same arguments, window,
+ * first tokens, cut lengths and scratch (vla_op_attention_kv8_scratch).  A visible key
+ * or value that is NaN gives NaN, one that is not visible reaches nothing. */
+size_t vla_op_attention_kv8_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
+vla_status vla_op_attention_kv8(const vla_heads *q, const void *cache, const int32_t *lens, const vla_heads *o, int B,
+                                int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,
+                                void *scratch, size_t scratch_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -130,6 +130,12 @@ def lib():
             "vla_op_w8_pack": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p],
             "vla_op_gemm_i8": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
                                c_int, c_int, c_void_p],
+            "vla_op_kv8_store": [c_char_p, c_char_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
+                                 c_void_p],
+            "vla_op_kv8_load": [c_void_p, c_void_p, c_void_p, c_char_p, c_char_p, c_int, c_int, c_int, c_int, c_int,
+                                c_void_p],
+            "vla_op_attention_kv8": [c_char_p, c_void_p, c_void_p, c_char_p, c_int, c_int, c_int, c_int, c_int, c_int,
+                                     c_int, c_int, c_int, c_void_p, c_size_t, c_void_p],
             "vla_suffix_create": [P(vla_stack_cfg), c_int, c_int, c_int, P(c_void_p)],
             "vla_suffix_load_block_weights": [c_void_p, c_int, P(vla_block_weights)],
             "vla_suffix_run": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
@@ -154,7 +160,7 @@ def lib():
         L.vla_op_packed_weight_elems.argtypes = [c_int, c_int]
         L.vla_op_packed_weight_elems.restype = c_size_t
         for name, n in (("vla_op_w4_packed_bytes", 3), ("vla_op_kv4_bytes", 4), ("vla_op_attention_kv4_scratch", 8),
-                        ("vla_op_w8_packed_bytes", 2)):
+                        ("vla_op_w8_packed_bytes", 2), ("vla_op_kv8_bytes", 4), ("vla_op_attention_kv8_scratch", 8)):
             getattr(L, name).argtypes = [c_int] * n
             getattr(L, name).restype = c_size_t
         L.vla_status_string.argtypes = [c_int]
@@ -532,6 +538,37 @@ def vla_op_gemm_i8(x, sx, Wp, residual, out, N, swiglu=False, stream=None):
     [M, N or N / 2] (float32 or bfloat16), rows of any stride; residual's rows
     and out's are equally far apart."""
     code = (_torch_ops or _ops()).gemm_i8(x, sx, Wp, residual, out, N, swiglu, stream)
+    if code:
+        _check(code)
+
+
+def vla_op_kv8_bytes(B, Hkv, L_cap, dh):
+    return lib().vla_op_kv8_bytes(B, Hkv, L_cap, dh)
+
+
+def vla_op_kv8_store(k, v, start, count, cache, L_cap, stream=None):
+    """k, v [B, L, Hkv, dh] bfloat16, start, count [B] int32 or None, cache a
+    tensor of vla_op_kv8_bytes(B, Hkv, L_cap, dh) bytes."""
+    code = (_torch_ops or _ops()).kv8_store(k, v, start, count, cache, L_cap, stream)
+    if code:
+        _check(code)
+
+
+def vla_op_kv8_load(cache, L_cap, start, count, k, v, stream=None):
+    """Rows out of the cache, into k and v."""
+    code = (_torch_ops or _ops()).kv8_load(k, v, start, count, cache, L_cap, stream)
+    if code:
+        _check(code)
+
+
+def vla_op_attention_kv8_scratch(B, Lq, H, Hkv, dh, max_len, window=0, sinks=0):
+    return lib().vla_op_attention_kv8_scratch(B, Lq, H, Hkv, dh, max_len, window, sinks)
+
+
+def vla_op_attention_kv8(q, cache, L_cap, Hkv, lens, o, max_len, window=0, sinks=0, scratch=None, stream=None):
+    """q, o [B, Lq, H, dh] bfloat16, lens [B] int32, scratch a tensor of
+    vla_op_attention_kv8_scratch(...) bytes (None where that is 0)."""
+    code = (_torch_ops or _ops()).attention_kv8(q, cache, L_cap, Hkv, lens, o, max_len, window, sinks, scratch, stream)
     if code:
         _check(code)
 

@@ -24,7 +24,7 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-fPIC", "-std=c++17", "-Xclang
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result"]
 
 SOURCES = ["gemm_bf16.hip", "attention_bf16.hip", "decode_bf16.hip", "norm.hip", "fp32_path.hip", "vision.hip",
-           "static_scratch.hip", "w4.hip", "qk_norm.hip", "kv4.hip", "norm_i8.hip", "w8.hip",
+           "static_scratch.hip", "w4.hip", "qk_norm.hip", "kv4.hip", "norm_i8.hip", "w8.hip", "kv8.hip",
            "runtime.cpp",
            "ops.cpp",
            "host_suffix.cpp", "host_suffix_api.cpp", "sched.cpp"]
@@ -33,6 +33,7 @@ SOURCES = ["gemm_bf16.hip", "attention_bf16.hip", "decode_bf16.hip", "norm.hip",
 EXTRA = {"attention_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          # the results of their MFMAs are scaled right after them
          "kv4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "w4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          # the host suffix executor: AVX-512 BF16 kernels, entered only after a CPU check
          "host_suffix.cpp": ["--offload-host-only", "-O3", "-mavx512f", "-mavx512bw", "-mavx512vl", "-mavx512bf16",
                              "-mfma"],

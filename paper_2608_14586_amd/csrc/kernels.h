@@ -256,6 +256,17 @@ size_t w8_packed_bytes(int N, int K);
 hipError_t w8_pack(const int8_t* codes, const float* scales, void* wp, int N, int K, hipStream_t s);
 hipError_t gemm_i8(const GemmI8Args& a, hipStream_t s);
 
+// Rows into and out of the 8-bit cache (kv8.hip), and attention over it: arguments as
+// of the 4-bit cache.
+using Kv8Rows = Kv4Rows;
+size_t kv8_bytes(int B, int Hkv, int L_cap, int dh);
+hipError_t kv8_store(Kv8Rows a, int dh, hipStream_t s);
+hipError_t kv8_load(Kv8Rows a, int dh, hipStream_t s);
+using Kv8Attn = Kv4Attn;
+size_t kv8_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
+// hipErrorOutOfMemory: a.part is smaller than kv8_attention_scratch
+hipError_t kv8_attention(Kv8Attn a, int dh, size_t scratch_bytes, hipStream_t s);
+
 // Fixed device scratch of the decode step that allocates nothing
 // (static_scratch.hip): its size, and its address on `device` (resolved once
 // per device; `device` must be the current device the first time).

@@ -74,6 +74,23 @@ vla_status attn_check(int B, int Lq, int H, int Hkv, int dh, int max_len, int* w
   if (*window == 0) *sinks = 0;
   return VLA_OK;
 }
+// the arguments of attention over a cache, 4-bit or 8-bit
+vla_status kv_attention(const vla_heads* q, const void* cache, const int32_t* lens, const vla_heads* o, int B, int Lq, int H,
+                        int Hkv, int L_cap, int dh, int max_len, int window, int sinks, void* scratch,
+                        size_t scratch_bytes, vla::Kv4Attn* a) {
+  if (!q || !o || B < 0 || Lq < 0 || !readable(*q, B, Lq) || !writable(*o, B, Lq, H) || (B && (!cache || !lens)))
+    return VLA_ERR_INVALID_ARG;
+  vla_status st = attn_check(B, Lq, H, Hkv, dh, max_len, &window, &sinks);
+  if (st == VLA_OK) st = kv4_check(B, Hkv, L_cap, dh);
+  if (st != VLA_OK) return st;
+  if (max_len > L_cap) return VLA_ERR_SHAPE;
+  if (!heads_ok(*q) || !heads_ok(*o) || !aligned(cache, 16) || !aligned(scratch, 16) || !aligned(lens, 4))
+    return VLA_ERR_UNSUPPORTED;
+  if (B && Lq && !scratch && scratch_bytes) return VLA_ERR_INVALID_ARG;
+  *a = vla::Kv4Attn{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks,
+                       0, 0, 0, {}, {}, {}, {}, 0.f};
+  return VLA_OK;
+}
 }  // namespace
 
 extern "C" {
@@ -237,18 +254,9 @@ size_t vla_op_attention_kv4_scratch(int B, int Lq, int H, int Hkv, int dh, int m
 vla_status vla_op_attention_kv4(const vla_heads* q, const void* cache, const int32_t* lens, const vla_heads* o, int B,
                                 int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,
                                 void* scratch, size_t scratch_bytes, void* stream) {
-  if (!q || !o || B < 0 || Lq < 0 || !readable(*q, B, Lq) || !writable(*o, B, Lq, H) || (B && (!cache || !lens)))
-    return VLA_ERR_INVALID_ARG;
-  vla_status st = attn_check(B, Lq, H, Hkv, dh, max_len, &window, &sinks);
-  if (st == VLA_OK) st = kv4_check(B, Hkv, L_cap, dh);
-  if (st != VLA_OK) return st;
-  if (max_len > L_cap) return VLA_ERR_SHAPE;
-  if (!heads_ok(*q) || !heads_ok(*o) || !aligned(cache, 16) || !aligned(scratch, 16) || !aligned(lens, 4))
-    return VLA_ERR_UNSUPPORTED;
-  if (B == 0 || Lq == 0) return VLA_OK;
-  if (!scratch && scratch_bytes) return VLA_ERR_INVALID_ARG;
-  const vla::Kv4Attn a{heads(*q), heads(*o), cache, lens, (float*)scratch, B, Lq, H, Hkv, L_cap, max_len, window, sinks,
-                       0, 0, 0, {}, {}, {}, {}, 0.f};
+  vla::Kv4Attn a;
+  const vla_status st = kv_attention(q, cache, lens, o, B, Lq, H, Hkv, L_cap, dh, max_len, window, sinks, scratch, scratch_bytes, &a);
+  if (st != VLA_OK || B == 0 || Lq == 0) return st;
   const hipError_t e = vla::kv4_attention(a, dh, scratch_bytes, (hipStream_t)stream);
   return e == hipErrorOutOfMemory ? VLA_ERR_SHAPE : status_of(e);
 }
@@ -302,6 +310,41 @@ vla_status vla_op_gemm_i8(const void* x, int64_t ldx, const float* sx, const voi
   const vla::GemmI8Args a{(const int8_t*)x, sx, (const uint8_t*)Wp, residual, out, M > 1 ? ldx : 0, M > 1 ? ldo : 0,
                           M, N, K, f32, swiglu != 0, whole};
   return status_of(vla::gemm_i8(a, (hipStream_t)stream));
+}
+
+size_t vla_op_kv8_bytes(int B, int Hkv, int L_cap, int dh) {
+  return kv4_check(B, Hkv, L_cap, dh) == VLA_OK ? vla::kv8_bytes(B, Hkv, L_cap, dh) : 0;
+}
+
+vla_status vla_op_kv8_store(const vla_heads* k, const vla_heads* v, const int32_t* start, const int32_t* count,
+                            void* cache, int B, int L, int Hkv, int L_cap, int dh, void* stream) {
+  vla::Kv8Rows a;
+  const vla_status st = kv4_rows(k, v, start, count, cache, B, L, Hkv, L_cap, dh, false, &a);
+  if (st != VLA_OK || B == 0 || L == 0) return st;
+  return status_of(vla::kv8_store(a, dh, (hipStream_t)stream));
+}
+
+vla_status vla_op_kv8_load(const void* cache, const int32_t* start, const int32_t* count, const vla_heads* k,
+                           const vla_heads* v, int B, int L, int Hkv, int L_cap, int dh, void* stream) {
+  vla::Kv8Rows a;
+  const vla_status st = kv4_rows(k, v, start, count, (void*)cache, B, L, Hkv, L_cap, dh, true, &a);
+  if (st != VLA_OK || B == 0 || L == 0) return st;
+  return status_of(vla::kv8_load(a, dh, (hipStream_t)stream));
+}
+
+size_t vla_op_attention_kv8_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks) {
+  if (attn_check(B, Lq, H, Hkv, dh, max_len, &window, &sinks) != VLA_OK || B == 0 || Lq == 0) return 0;
+  return vla::kv8_attention_scratch(B, Lq, H, Hkv, dh, max_len, window, sinks);
+}
+
+vla_status vla_op_attention_kv8(const vla_heads* q, const void* cache, const int32_t* lens, const vla_heads* o, int B,
+                                int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,
+                                void* scratch, size_t scratch_bytes, void* stream) {
+  vla::Kv8Attn a;
+  const vla_status st = kv_attention(q, cache, lens, o, B, Lq, H, Hkv, L_cap, dh, max_len, window, sinks, scratch, scratch_bytes, &a);
+  if (st != VLA_OK || B == 0 || Lq == 0) return st;
+  const hipError_t e = vla::kv8_attention(a, dh, scratch_bytes, (hipStream_t)stream);
+  return e == hipErrorOutOfMemory ? VLA_ERR_SHAPE : status_of(e);
 }
 
 }  // extern "C"

@@ -204,7 +204,8 @@ vla_status qk_norm_rope(PyObject* const* a) {
 }
 
 // args: k, v, start, count, cache, L_cap, stream
-vla_status kv4_rows(PyObject* const* a, bool load) {
+template <size_t (*BYTES)(int, int, int, int), auto STORE, auto LOAD>
+vla_status kv_rows(PyObject* const* a, bool load) {
   const at::Tensor &k = tensor_of(a[0], "k"), &v = tensor_of(a[1], "v");
   const int dev = device_of(k, "k"), cap = int_of(a[5], "L_cap");
   four(k, "k");
@@ -212,15 +213,20 @@ vla_status kv4_rows(PyObject* const* a, bool load) {
   const vla_heads kh = heads(k, BF16, k.sizes(), dev, "k"), vh = heads(v, BF16, k.sizes(), dev, "v");
   const int64_t bs[1] = {B};
   const int32_t *start = (int32_t*)dense(a[2], I32, bs, dev, "start"), *count = (int32_t*)dense(a[3], I32, bs, dev, "count");
-  void* cache = memory(a[4], vla_op_kv4_bytes(B, Hkv, cap, dh), dev, "cache");
-  return load ? vla_op_kv4_load(cache, start, count, &kh, &vh, B, L, Hkv, cap, dh, stream_of(a[6]))
-              : vla_op_kv4_store(&kh, &vh, start, count, cache, B, L, Hkv, cap, dh, stream_of(a[6]));
+  void* cache = memory(a[4], BYTES(B, Hkv, cap, dh), dev, "cache");
+  return load ? LOAD(cache, start, count, &kh, &vh, B, L, Hkv, cap, dh, stream_of(a[6]))
+              : STORE(&kh, &vh, start, count, cache, B, L, Hkv, cap, dh, stream_of(a[6]));
 }
+constexpr auto kv4_rows = kv_rows<vla_op_kv4_bytes, vla_op_kv4_store, vla_op_kv4_load>;
+constexpr auto kv8_rows = kv_rows<vla_op_kv8_bytes, vla_op_kv8_store, vla_op_kv8_load>;
 vla_status kv4_store(PyObject* const* a) { return kv4_rows(a, false); }
 vla_status kv4_load(PyObject* const* a) { return kv4_rows(a, true); }
+vla_status kv8_store(PyObject* const* a) { return kv8_rows(a, false); }
+vla_status kv8_load(PyObject* const* a) { return kv8_rows(a, true); }
 
 // args: q, cache, L_cap, Hkv, lens, o, max_len, window, sinks, scratch, stream
-vla_status attention_kv4(PyObject* const* a) {
+template <size_t (*BYTES)(int, int, int, int), auto ATTENTION>
+vla_status attention_kv(PyObject* const* a) {
   const at::Tensor& q = tensor_of(a[0], "q");
   const int dev = device_of(q, "q"), cap = int_of(a[2], "L_cap"), Hkv = int_of(a[3], "Hkv");
   four(q, "q");
@@ -231,11 +237,12 @@ vla_status attention_kv4(PyObject* const* a) {
   if (a[4] == Py_None) throw Misfit{"lens", "int32 [B]"};
   size_t bytes = 0;
   void* scratch = a[9] == Py_None ? nullptr : memory(a[9], 0, dev, "scratch", &bytes);
-  return vla_op_attention_kv4(&qh, memory(a[1], vla_op_kv4_bytes(B, Hkv, cap, dh), dev, "cache"),
-                              (int32_t*)dense(a[4], I32, bs, dev, "lens"), &oh, B, Lq, H, Hkv, cap, dh,
-                              int_of(a[6], "max_len"), int_of(a[7], "window"), int_of(a[8], "sinks"),
-                              bytes ? scratch : nullptr, bytes, stream_of(a[10]));
+  return ATTENTION(&qh, memory(a[1], BYTES(B, Hkv, cap, dh), dev, "cache"), (int32_t*)dense(a[4], I32, bs, dev, "lens"),
+                   &oh, B, Lq, H, Hkv, cap, dh, int_of(a[6], "max_len"), int_of(a[7], "window"), int_of(a[8], "sinks"),
+                   bytes ? scratch : nullptr, bytes, stream_of(a[10]));
 }
+constexpr auto attention_kv4 = attention_kv<vla_op_kv4_bytes, vla_op_attention_kv4>;
+constexpr auto attention_kv8 = attention_kv<vla_op_kv8_bytes, vla_op_attention_kv8>;
 
 // args: x, add, sum, g, eps, codes, scales, stream
 vla_status norm_i8(PyObject* const* a) {
@@ -330,6 +337,9 @@ PyMethodDef methods[] = {method<w4_pack, 6>("w4_pack"),
                          method<norm_i8, 8>("norm_i8"),
                          method<w8_pack, 4>("w8_pack"),
                          method<gemm_i8, 8>("gemm_i8"),
+                         method<kv8_store, 7>("kv8_store"),
+                         method<kv8_load, 7>("kv8_load"),
+                         method<attention_kv8, 11>("attention_kv8"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
