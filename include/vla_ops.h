@@ -233,6 +233,17 @@ vla_status vla_op_w8_pack(const void *codes, const float *scales, void *Wp, int 
 vla_status vla_op_gemm_i8(const void *x, int64_t ldx, const float *sx, const void *Wp, const float *residual, void *out,
                           int64_t ldo, vla_dtype out_dtype, int swiglu, int M, int N, int K, void *stream);
 
+/* Causal attention inside each of n_seq packed prompts: prompt i is rows
+ * [offsets[i], offsets[i + 1]) of q[T][H][dh], k, v[T][Hkv][dh] and o[T][H][dh] (bf16;
+ * the seq stride of the vla_heads is not used), and row t of it gets softmax(q_t k_j /
+ * sqrt(dh)) v_j over its rows j <= t, query head h reading KV head h / (H / Hkv).
+ * offsets[n_seq + 1] (device int32) do not fall; those outside [0, T] are cut.  A
+ * prompt may have no rows.  Rows of o in no prompt stay as they were, rows of q, k, v
+ * in none may hold anything, and no prompt's values reach another's.
+ * dh in {64, 128}, H % Hkv == 0, token strides below 2^24. */
+vla_status vla_op_attention_packed(const vla_heads *q, const vla_heads *k, const vla_heads *v, const int32_t *offsets,
+                                   const vla_heads *o, int n_seq, int T, int H, int Hkv, int dh, void *stream);
+
 /* A KV cache of 8 bits a value for B sequences of up to L_cap tokens:
  * vla_op_kv8_bytes bytes of device memory (16-byte aligned), opaque within.  32
  * positions of a head (from a multiple of 32 on) are a block; the block's keys share a

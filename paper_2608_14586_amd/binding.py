@@ -130,6 +130,8 @@ def lib():
             "vla_op_w8_pack": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p],
             "vla_op_gemm_i8": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
                                c_int, c_int, c_void_p],
+            "vla_op_attention_packed": [c_char_p, c_char_p, c_char_p, c_void_p, c_char_p, c_int, c_int, c_int, c_int,
+                                        c_int, c_void_p],
             "vla_op_kv8_store": [c_char_p, c_char_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
                                  c_void_p],
             "vla_op_kv8_load": [c_void_p, c_void_p, c_void_p, c_char_p, c_char_p, c_int, c_int, c_int, c_int, c_int,
@@ -538,6 +540,14 @@ def vla_op_gemm_i8(x, sx, Wp, residual, out, N, swiglu=False, stream=None):
     [M, N or N / 2] (float32 or bfloat16), rows of any stride; residual's rows
     and out's are equally far apart."""
     code = (_torch_ops or _ops()).gemm_i8(x, sx, Wp, residual, out, N, swiglu, stream)
+    if code:
+        _check(code)
+
+
+def vla_op_attention_packed(q, k, v, offsets, o, stream=None):
+    """q, o [T, H, dh], k, v [T, Hkv, dh] bfloat16, rows of any stride, offsets
+    [prompts + 1] int32: causal attention inside each prompt."""
+    code = (_torch_ops or _ops()).attention_packed(q, k, v, offsets, o, stream)
     if code:
         _check(code)
 

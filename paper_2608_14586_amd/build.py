@@ -24,13 +24,14 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-fPIC", "-std=c++17", "-Xclang
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result"]
 
 SOURCES = ["gemm_bf16.hip", "attention_bf16.hip", "decode_bf16.hip", "norm.hip", "fp32_path.hip", "vision.hip",
-           "static_scratch.hip", "w4.hip", "qk_norm.hip", "kv4.hip", "norm_i8.hip", "w8.hip", "kv8.hip",
+           "static_scratch.hip", "w4.hip", "qk_norm.hip", "kv4.hip", "norm_i8.hip", "w8.hip", "kv8.hip", "attention_packed.hip",
            "runtime.cpp",
            "ops.cpp",
            "host_suffix.cpp", "host_suffix_api.cpp", "sched.cpp"]
 # Attention keeps its score and output accumulators in VGPRs: the softmax
 # touches them every key tile, and AGPR accumulators would cost a copy each way.
 EXTRA = {"attention_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "attention_packed.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          # the results of their MFMAs are scaled right after them
          "kv4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "w4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],

@@ -256,6 +256,18 @@ size_t w8_packed_bytes(int N, int K);
 hipError_t w8_pack(const int8_t* codes, const float* scales, void* wp, int N, int K, hipStream_t s);
 hipError_t gemm_i8(const GemmI8Args& a, hipStream_t s);
 
+// Causal attention inside each of n_seq packed prompts, rows [offsets[i], offsets[i +
+// 1]) of T (attention_packed.hip); what comes after Hkv is filled in by the launch.
+struct PackedAttn {
+  Heads q, k, v, o;  // seq is not used
+  const int32_t* offsets;
+  int n_seq, T, H, Hkv;
+  int G;  // query heads a KV head
+  FastDiv by_H, by_Hkv;
+  float scale_log2;
+};
+hipError_t attention_packed(PackedAttn a, int dh, hipStream_t s);
+
 // Rows into and out of the 8-bit cache (kv8.hip), and attention over it: arguments as
 // of the 4-bit cache.
 using Kv8Rows = Kv4Rows;

@@ -312,6 +312,21 @@ vla_status vla_op_gemm_i8(const void* x, int64_t ldx, const float* sx, const voi
   return status_of(vla::gemm_i8(a, (hipStream_t)stream));
 }
 
+vla_status vla_op_attention_packed(const vla_heads* q, const vla_heads* k, const vla_heads* v, const int32_t* offsets,
+                                   const vla_heads* o, int n_seq, int T, int H, int Hkv, int dh, void* stream) {
+  if (!q || !k || !v || !o || n_seq < 0 || T < 0 || H <= 0 || Hkv <= 0 || (n_seq && !offsets) || !readable(*q, 1, T) ||
+      !readable(*k, 1, T) || !readable(*v, 1, T) || !writable(*o, 1, T, H))
+    return VLA_ERR_INVALID_ARG;
+  if (H % Hkv || (dh != 64 && dh != 128) || !heads_ok(*q) || !heads_ok(*k) || !heads_ok(*v) || !heads_ok(*o) ||
+      !aligned(offsets, 4))
+    return VLA_ERR_UNSUPPORTED;
+  // 64 rows of keys and values lie within 2^31 bytes
+  if (k->token >= 1 << 24 || v->token >= 1 << 24) return VLA_ERR_UNSUPPORTED;
+  if (n_seq == 0 || T == 0) return VLA_OK;
+  const vla::PackedAttn a{heads(*q), heads(*k), heads(*v), heads(*o), offsets, n_seq, T, H, Hkv, 0, {}, {}, 0.f};
+  return status_of(vla::attention_packed(a, dh, (hipStream_t)stream));
+}
+
 size_t vla_op_kv8_bytes(int B, int Hkv, int L_cap, int dh) {
   return kv4_check(B, Hkv, L_cap, dh) == VLA_OK ? vla::kv8_bytes(B, Hkv, L_cap, dh) : 0;
 }

@@ -203,6 +203,33 @@ vla_status qk_norm_rope(PyObject* const* a) {
                              (int32_t*)dense(a[7], I32, ps, dev, "pos"), &qo, &ko, B, L, H, Hkv, dh, stream_of(a[10]));
 }
 
+// [T, heads, dh], any outer strides
+vla_heads packed_heads(PyObject* o, at::IntArrayRef shape, int device, const char* name) {
+  const at::Tensor& t = tensor_of(o, name);
+  on(t, device, name);
+  if (t.scalar_type() != BF16 || t.sizes() != shape || (t.stride(2) != 1 && t.size(2) != 1))
+    throw Misfit{name, "bfloat16 of the shape that the call's other sizes give, its last dimension dense"};
+  auto stride = [&](int d) { return t.size(d) == 1 ? 0 : t.stride(d); };
+  return vla_heads{t.data_ptr(), 0, stride(0), stride(1)};
+}
+
+// args: q, k, v, offsets, o, stream
+vla_status attention_packed(PyObject* const* a) {
+  const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k"), &off = tensor_of(a[3], "offsets");
+  const int dev = device_of(q, "q");
+  if (q.dim() != 3) throw Misfit{"q", "three dimensions"};
+  if (k.dim() != 3) throw Misfit{"k", "three dimensions"};
+  const int T = dim(q, 0, "q"), H = dim(q, 1, "q"), dh = dim(q, 2, "q"), Hkv = dim(k, 1, "k");
+  const int64_t ks[3] = {T, Hkv, dh};
+  const vla_heads qh = packed_heads(a[0], q.sizes(), dev, "q"), kh = packed_heads(a[1], ks, dev, "k");
+  const vla_heads vh = packed_heads(a[2], ks, dev, "v"), oh = packed_heads(a[4], q.sizes(), dev, "o");
+  on(off, dev, "offsets");
+  if (off.dim() != 1 || off.scalar_type() != I32 || !off.is_contiguous() || off.size(0) < 1)
+    throw Misfit{"offsets", "contiguous int32 [prompts + 1]"};
+  return vla_op_attention_packed(&qh, &kh, &vh, (int32_t*)off.data_ptr(), &oh, dim(off, 0, "offsets") - 1, T, H, Hkv, dh,
+                                 stream_of(a[5]));
+}
+
 // args: k, v, start, count, cache, L_cap, stream
 template <size_t (*BYTES)(int, int, int, int), auto STORE, auto LOAD>
 vla_status kv_rows(PyObject* const* a, bool load) {
@@ -337,6 +364,7 @@ PyMethodDef methods[] = {method<w4_pack, 6>("w4_pack"),
                          method<norm_i8, 8>("norm_i8"),
                          method<w8_pack, 4>("w8_pack"),
                          method<gemm_i8, 8>("gemm_i8"),
+                         method<attention_packed, 6>("attention_packed"),
                          method<kv8_store, 7>("kv8_store"),
                          method<kv8_load, 7>("kv8_load"),
                          method<attention_kv8, 11>("attention_kv8"),
