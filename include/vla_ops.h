@@ -232,6 +232,9 @@ vla_status vla_op_w8_pack(const void *codes, const float *scales, void *Wp, int 
  * not finite, and reaches no other row. */
 vla_status vla_op_gemm_i8(const void *x, int64_t ldx, const float *sx, const void *Wp, const float *residual, void *out,
                           int64_t ldo, vla_dtype out_dtype, int swiglu, int M, int N, int K, void *stream);
+/* How such a product runs, for tests and timings (host only, no GPU work): in
+ * tiles of tile[0] rows of x by tile[1] of W; zeros: by the kernel of up to 16 rows. */
+vla_status vla_op_gemm_i8_tile(int M, int N, int K, int tile[2]);
 
 /* Causal attention inside each of n_seq packed prompts: prompt i is rows
  * [offsets[i], offsets[i + 1]) of q[T][H][dh], k, v[T][Hkv][dh] and o[T][H][dh] (bf16;

@@ -130,6 +130,7 @@ def lib():
             "vla_op_w8_pack": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p],
             "vla_op_gemm_i8": [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int, c_int, c_int,
                                c_int, c_int, c_void_p],
+            "vla_op_gemm_i8_tile": [c_int, c_int, c_int, P(c_int)],
             "vla_op_attention_packed": [c_char_p, c_char_p, c_char_p, c_void_p, c_char_p, c_int, c_int, c_int, c_int,
                                         c_int, c_void_p],
             "vla_op_kv8_store": [c_char_p, c_char_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
@@ -542,6 +543,13 @@ def vla_op_gemm_i8(x, sx, Wp, residual, out, N, swiglu=False, stream=None):
     code = (_torch_ops or _ops()).gemm_i8(x, sx, Wp, residual, out, N, swiglu, stream)
     if code:
         _check(code)
+
+
+def vla_op_gemm_i8_tile(M, N, K):
+    """(rows, columns) of the tiles in which the product runs; (0, 0): the kernel of up to 16 rows."""
+    t = (c_int * 2)()
+    _check(lib().vla_op_gemm_i8_tile(M, N, K, t))
+    return tuple(t)
 
 
 def vla_op_attention_packed(q, k, v, offsets, o, stream=None):

@@ -255,6 +255,8 @@ struct GemmI8Args {
 size_t w8_packed_bytes(int N, int K);
 hipError_t w8_pack(const int8_t* codes, const float* scales, void* wp, int N, int K, hipStream_t s);
 hipError_t gemm_i8(const GemmI8Args& a, hipStream_t s);
+// the tile in which it runs, zeros for the kernel of up to 16 rows
+void gemm_i8_tile(int M, int N, int K, int* rows, int* cols);
 
 // Causal attention inside each of n_seq packed prompts, rows [offsets[i], offsets[i +
 // 1]) of T (attention_packed.hip); what comes after Hkv is filled in by the launch.

@@ -312,6 +312,13 @@ vla_status vla_op_gemm_i8(const void* x, int64_t ldx, const float* sx, const voi
   return status_of(vla::gemm_i8(a, (hipStream_t)stream));
 }
 
+vla_status vla_op_gemm_i8_tile(int M, int N, int K, int* tile) {
+  if (!tile || M <= 0) return VLA_ERR_INVALID_ARG;
+  const vla_status st = w8_check(N, K);
+  if (st == VLA_OK) vla::gemm_i8_tile(M, N, K, &tile[0], &tile[1]);
+  return st;
+}
+
 vla_status vla_op_attention_packed(const vla_heads* q, const vla_heads* k, const vla_heads* v, const int32_t* offsets,
                                    const vla_heads* o, int n_seq, int T, int H, int Hkv, int dh, void* stream) {
   if (!q || !k || !v || !o || n_seq < 0 || T < 0 || H <= 0 || Hkv <= 0 || (n_seq && !offsets) || !readable(*q, 1, T) ||

@@ -95,19 +95,18 @@ __device__ __forceinline__ void by_output(const GemmI8Args& a, F f) {
 
 // ------------------------------------------------------------------ few rows
 //
-// Up to 16 MT rows of x: the weights' bytes are the bound.  A workgroup takes NT
-// tiles of weight rows (SWIGLU: NT / 2 gate tiles and the up tiles of the same
-// features); its W waves take runs of U steps in turn and add up in LDS.  Weights go
-// from memory into registers, a run ahead.
-template <int NT, int MT, int W, int U, bool SWIGLU>
+// Up to 16 rows of x: the weights' bytes are the bound.  A workgroup takes NT tiles of
+// weight rows (SWIGLU: NT / 2 gate tiles and the up tiles of the same features); its W
+// waves take runs of U steps in turn and add up in LDS.  Weights and x go from memory
+// into registers, a run ahead.
+template <int NT, int W, int U, bool SWIGLU>
 __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
-  __shared__ i32x4 part[W][NT * MT][64];
+  __shared__ i32x4 part[W][NT][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, q = lane >> 4;
   const int KS = steps_of(a.K), ntiles = tiles_of(a.N), half = ntiles / 2;
   constexpr int TW = SWIGLU ? NT / 2 : NT;
-  const int t0 = blockIdx.x * TW, m0 = blockIdx.y * (16 * MT);
-  const int rows = min(a.M - m0, 16 * MT);
+  const int t0 = blockIdx.x * TW;
   const uint8_t* wt[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
@@ -115,45 +114,33 @@ __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
     wt[i] = a.wp + (size_t)t * KS * 1024;
   }
   // past the row of x: its next one, or zeros past the last; the weights there are zero
-  const uint8_t* xp = (const uint8_t*)a.x + (int64_t)m0 * a.ldx;
-  const uint32_t xbytes = (uint32_t)((rows - 1) * a.ldx + a.K);
-  uint32_t xat[MT];
-#pragma unroll
-  for (int j = 0; j < MT; ++j) {
-    const int r = j * 16 + c16;
-    xat[j] = r < rows ? (uint32_t)(r * a.ldx) + q * 16 : 0x80000000u;
-  }
-  i32x4 wr[2][NT][U], xr[2][MT][U];
+  const uint32_t xbytes = (uint32_t)((a.M - 1) * a.ldx + a.K);
+  const uint32_t xat = c16 < a.M ? (uint32_t)(c16 * a.ldx) + q * 16 : NOWHERE;
+  i32x4 wr[2][NT][U], xr[2][U];
   auto fetch = [&](int b, int s0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool in = s0 + u < KS;
+      const bool in = s0 + u < KS;  // past the last step: empty buffers, no memory is touched
 #pragma unroll
       for (int i = 0; i < NT; ++i)
         wr[b][i][u] = __builtin_bit_cast(
             i32x4, __builtin_amdgcn_raw_buffer_load_b128(
                        __builtin_amdgcn_make_buffer_rsrc((void*)wt[i], (short)0, in ? KS * 1024 : 0, 0x00020000),
                        lane * 16, in ? (s0 + u) * 1024 : 0, 0));
-#pragma unroll
-      for (int j = 0; j < MT; ++j)
-        xr[b][j][u] = __builtin_bit_cast(
-            i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                       __builtin_amdgcn_make_buffer_rsrc((void*)xp, (short)0, in ? (int)xbytes : 0, 0x00020000), xat[j],
-                       in ? (s0 + u) * 64 : 0, 0));
+      xr[b][u] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     __builtin_amdgcn_make_buffer_rsrc((void*)a.x, (short)0, in ? (int)xbytes : 0, 0x00020000), xat,
+                     in ? (s0 + u) * 64 : 0, 0));
     }
   };
-  i32x4 acc[NT][MT];
+  i32x4 acc[NT];
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int j = 0; j < MT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  for (int i = 0; i < NT; ++i) acc[i] = i32x4{0, 0, 0, 0};
   auto multiply = [&](int b) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] = mfma_i8(wr[b][i][u], xr[b][j][u], acc[i][j]);
+      for (int i = 0; i < NT; ++i) acc[i] = mfma_i8(wr[b][i][u], xr[b][u], acc[i]);
   };
   int s = wave * U;
   fetch(0, s);
@@ -169,107 +156,112 @@ __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
     s += W * U;
   }
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int j = 0; j < MT; ++j) part[wave][i * MT + j][lane] = acc[i][j];
+  for (int i = 0; i < NT; ++i) part[wave][i][lane] = acc[i];
   __syncthreads();
   const float* sw = (const float*)(a.wp + code_bytes(a.N, a.K));
   const int N = SWIGLU ? a.N / 2 : a.N;
-  for (int e = wave; e < TW * MT; e += W) {
-    const int i = e / MT, j = e % MT;
-    const int m = j * 16 + c16, t = min(t0 + i, (SWIGLU ? half : ntiles) - 1), col = row_of(t0 + i, 4 * q);
+  for (int i = wave; i < TW; i += W) {
+    const int t = min(t0 + i, (SWIGLU ? half : ntiles) - 1), col = row_of(t0 + i, 4 * q);
     auto joined = [&](int i) {
-      i32x4 v = part[0][i * MT + j][lane];
+      i32x4 v = part[0][i][lane];
 #pragma unroll
-      for (int w = 1; w < W; ++w) v += part[w][i * MT + j][lane];
+      for (int w = 1; w < W; ++w) v += part[w][i][lane];
       return v;
     };
-    const i32x4 v = joined(i), g = SWIGLU ? joined(i + TW) : v;
-    const float sx = a.sx[m0 + min(m, rows - 1)];
-    const f32x4 ws = *(const f32x4*)(sw + t * 16 + q * 4);  
+    const i32x4 v = joined(i), u = SWIGLU ? joined(i + TW) : v;
+    const float sx = a.sx[min(c16, a.M - 1)];
+    const f32x4 ws = *(const f32x4*)(sw + t * 16 + q * 4);
     f32x4 y;
 #pragma unroll
     for (int x = 0; x < 4; ++x) y[x] = (float)v[x] * sx * ws[x];
     if constexpr (SWIGLU) {
       const f32x4 us = *(const f32x4*)(sw + (half + t) * 16 + q * 4);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) y[x] = silu_of(y[x]) * ((float)g[x] * sx * us[x]);
+      for (int x = 0; x < 4; ++x) y[x] = silu_of(y[x]) * ((float)u[x] * sx * us[x]);
     }
     by_output(a, [&](auto wide, auto f32) {
-      const Rows<wide.value, f32.value> io(a, m0, rows, N);
-      const uint32_t at = m * (uint32_t)a.ldo + col;
-      if (a.res) y += io.residual(at, col, m < rows);
-      io.store(at, col, m < rows, y);
+      const Rows<wide.value, f32.value> io(a, 0, a.M, N);
+      const uint32_t at = c16 * (uint32_t)a.ldo + col;
+      if (a.res) y += io.residual(at, col, c16 < a.M);
+      io.store(at, col, c16 < a.M, y);
     });
   }
 }
 
 // ----------------------------------------------------------------- many rows
 //
-// A workgroup of 64 NW threads takes BM rows of x by BN rows of W.  Slabs of KG
-// steps of 64 k move to LDS by buffer_load ... lds in a ring of NS stages, both
-// operands in MFMA order (1024 bytes a tile and step, lane l's operand at 16 l), so
-// that every read of an operand is 64 lanes side by side, free of bank conflicts
-// without a swizzle.  While the MFMAs of slab i run, its successor's operands are
-// read into registers and slab i + NS is on its way into the stage that slab i left.
-// KG = 2: half of the waves take the even steps, half the odd ones, and add up in LDS.
-template <int BM, int BN, int WGM, int WGN, int KG, int NS, bool SWIGLU>
-__global__ __launch_bounds__(64 * WGM * WGN * KG) void w8_tile_kernel(GemmI8Args a) {
-  constexpr int NW = WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
-  constexpr int AB = BM / 16 * KG, WB = BN / 16 * KG, PA = AB / NW, PW = WB / NW, PER = PA + PW;  // 1 KB blocks
-  constexpr int STAGE = (AB + WB) * 1024;
-  static_assert(PA * NW == AB && PW * NW == WB, "blocks divide over the waves");
-  static_assert((NS - 2) * PER < 64, "vmcnt range");
-  static_assert(!SWIGLU || WN % 64 == 0, "a wave's tiles must be whole (gate, up) groups");
-  constexpr int RED = KG > 1 ? WGM * WGN * TM * TN * 1024 : 0;
-  __shared__ __attribute__((aligned(1024))) char smem[NS * STAGE > RED ? NS * STAGE : RED];
+// A workgroup of WGN KG waves takes BM rows of x by BN rows of W, each wave all BM rows by
+// BN / WGN (KG = 2: two waves of them, one for the even steps of 64 k and one for the odd
+// ones, joined in LDS at the end).  Weights go from memory straight into the registers of the
+// one wave that multiplies them, D steps ahead.  x goes to LDS by buffer_load ... lds, two
+// steps (a slab) at a time into a ring of NX, and is read LA operands ahead of the
+// MFMAs that take it, so a slab costs one barrier.
+//
+// What bounds it is how fast a CU is filled, 70 GB/s or 33 bytes a cycle in whole cache
+// lines: (BM + BN) 64 bytes a step against BM BN / 64 cycles of MFMAs (8192 operations a
+// cycle and CU).  With 64 bytes of a row of x a load, in place of the 128 of a cache line,
+// x counted twice (333 x 4096, K = 11008 38 us, now 29).
+template <int BM, int BN, int WGN, int KG, int NX, int D, int LA, bool SWIGLU>
+__global__ __launch_bounds__(64 * WGN * KG) void w8_tile_kernel(GemmI8Args a) {
+  constexpr int NW = WGN * KG, TM = BM / 16, TN = BN / WGN / 16, SP = 2 / KG;  // own steps a slab
+  constexpr int XB = BM / 8, PX = (XB + NW - 1) / NW, XS = XB * 1024;            // 1 KB loads of a slab of x
+  static_assert(PX == 1 || (PX % 2 == 0 && PX * NW == XB), "a load's half of 16 rows is known");
+  static_assert(TM % LA == 0 && D % SP == 0 && (NX - 1) * PX + D * TN < 64, "unrolling, vmcnt range");
+  static_assert(!SWIGLU || TN % 2 == 0, "a wave's tiles must be whole (gate, up) pairs");
+  constexpr int RED = KG > 1 ? WGN * TM * TN * 1024 : 0;
+  __shared__ __attribute__((aligned(1024))) char smem[NX * XS > RED ? NX * XS : RED];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kg = wave / (WGM * WGN), wm = wave / WGN % WGM, wn = wave % WGN;
+  const int kg = wave / WGN, wn = wave % WGN;
   const int c16 = lane & 15, q = lane >> 4;
   const int KS = steps_of(a.K), ntiles = tiles_of(a.N), half = ntiles / 2;
-  const int nslab = KS / KG;
 
   // tiles: each of the 8 XCDs takes a contiguous run of them, walked M first inside
   // groups of 8 tile rows
   const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
-  const int nwg = gridDim.x;
   int id = blockIdx.x;
   {
-    const int per = nwg >> 3, rem = nwg & 7, x = id & 7;
+    const int per = gridDim.x >> 3, rem = gridDim.x & 7, x = id & 7;
     id = x * per + min(x, rem) + (id >> 3);
   }
   const int group = 8 * tiles_n, first_m = id / group * 8, gsz = min(tiles_m - first_m, 8);
   const int m0 = (first_m + id % group % gsz) * BM, tile_n = id % group / gsz;
-  const int t0 = SWIGLU ? tile_n * (BN / 32) : tile_n * (BN / 16);  // first tile of W (of the gate's)
-
   const int rows = min(a.M - m0, BM);
+
+  // x: 8 rows of 128 bytes a load; of 16 rows, row r has its 16-byte chunk c at c ^ (r / 2)
+  // of 128, so that 16 rows of one chunk meet every bank alike
   const uint8_t* xp = (const uint8_t*)a.x + (int64_t)m0 * a.ldx;
   const int xbytes = (int)((rows - 1) * a.ldx + a.K);
-  const uint8_t* wp0 = a.wp + (size_t)t0 * KS * 1024;
-  const uint8_t* wp1 = SWIGLU ? a.wp + (size_t)(half + t0) * KS * 1024 : wp0;
-  const int wt = min((SWIGLU ? half : ntiles) - t0, SWIGLU ? BN / 32 : BN / 16);
-  const int wbytes = wt * KS * 1024;
-
-  // this wave's blocks of a slab: x block j is tile (wave PA + j) / KG, step (wave PA + j) % KG
-  const uint32_t xvoff = (uint32_t)(c16 * a.ldx) + q * 16, wvoff = lane * 16;
-  auto issue = [&](int slab, char* st) {
-    const bool in = slab < nslab;  // past the last: empty buffers, no memory touched
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)xp, (short)0, in ? xbytes : 0, 0x00020000);
+  uint32_t xvoff[2];
 #pragma unroll
-    for (int j = 0; j < PA; ++j) {
-      const int blk = wave * PA + j, t = blk / KG, s = blk % KG;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void*)(st + blk * 1024), 16, xvoff,
-                                               (int)(t * 16 * a.ldx) + (slab * KG + s) * 64, 0, 0);
+  for (int h = 0; h < 2; ++h)
+    xvoff[h] = (uint32_t)((lane >> 3) * a.ldx) + ((lane & 7) ^ (4 * (PX == 1 ? wave & 1 : h) + (lane >> 4))) * 16;
+  auto issue_x = [&](int slab, char* st) {
+    // past the last slab: an empty buffer, no memory is touched
+    const __amdgpu_buffer_rsrc_t rx =
+        __builtin_amdgcn_make_buffer_rsrc((void*)xp, (short)0, 2 * slab < KS ? xbytes : 0, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < PX; ++j) {
+      const int blk = wave * PX + j;
+      if (PX * NW == XB || blk < XB)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void*)(st + blk * 1024), 16,
+                                                 xvoff[j & 1], (int)(blk * 8 * a.ldx) + slab * 128, 0, 0);
     }
+  };
+  // W: SWIGLU takes gate and up tiles of the same features in turn
+  const int t0 = SWIGLU ? tile_n * (BN / 32) : tile_n * (BN / 16);  // first tile of W (of the gate's)
+  const int wt = min((SWIGLU ? half : ntiles) - t0, SWIGLU ? BN / 32 : BN / 16);
+  const uint8_t* wp[2] = {a.wp + (size_t)t0 * KS * 1024, a.wp + (size_t)((SWIGLU ? half : 0) + t0) * KS * 1024};
+  const int wbytes = wt * KS * 1024;  // tiles past W read as zero
+  i32x4 w[D][TN];
+  auto fetch = [&](int own, int d) {
+    const int s = KG == 1 ? own : 2 * own + kg;
 #pragma unroll
-    for (int j = 0; j < PW; ++j) {
-      const int blk = wave * PW + j, t = blk / KG, s = blk % KG;
-      // SWIGLU: two gate tiles, then the two up tiles of the same features
-      const bool up = SWIGLU && (t & 2);
-      const int tt = SWIGLU ? (t >> 2) * 2 + (t & 1) : t;
-      const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)(up ? wp1 : wp0), (short)0, in ? wbytes : 0, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void*)(st + (AB + blk) * 1024), 16,
-                                               wvoff, (tt * KS + slab * KG + s) * 1024, 0, 0);
+    for (int n = 0; n < TN; ++n) {
+      const int x = wn * TN + n, t = SWIGLU ? x >> 1 : x;
+      w[d][n] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     __builtin_amdgcn_make_buffer_rsrc((void*)wp[SWIGLU ? n & 1 : 0], (short)0, s < KS ? wbytes : 0, 0x00020000),
+                     lane * 16, (t * KS + s) * 1024, 0));
     }
   };
 
@@ -278,14 +270,10 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG) void w8_tile_kernel(GemmI8Args
   for (int n = 0; n < TN; ++n)
 #pragma unroll
     for (int m = 0; m < TM; ++m) acc[n][m] = i32x4{0, 0, 0, 0};
-  i32x4 fx[2][TM], fw[2][TN];
-  const int xread = (wm * TM * KG + kg) * 1024 + lane * 16, wread = (AB + wn * TN * KG + kg) * 1024 + lane * 16;
-  auto read = [&](const char* st, int i, int b) {
-    if (i < TN)
-      fw[b][i] = *(const i32x4*)(st + wread + i * KG * 1024);
-    else
-      fx[b][i - TN] = *(const i32x4*)(st + xread + (i - TN) * KG * 1024);
-  };
+  i32x4 fx[LA];
+  const int xr = c16 * 128;
+  // of the own step p of a slab
+  const int xc[2] = {((KG == 1 ? 0 : 4 * kg) + q ^ (c16 >> 1)) * 16, (4 + q ^ (c16 >> 1)) * 16};
   auto wait = [](auto n) {
     constexpr int N = decltype(n)::value;
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);  // vmcnt(N), lgkmcnt(0)
@@ -293,39 +281,51 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG) void w8_tile_kernel(GemmI8Args
     asm volatile("" ::: "memory");
   };
 #pragma unroll
-  for (int i = 0; i < NS; ++i) issue(i, smem + i * STAGE);
-  wait(std::integral_constant<int, (NS - 1) * PER>{});
+  for (int i = 0; i < NX - 1; ++i) issue_x(i, smem + i * XS);
 #pragma unroll
-  for (int i = 0; i < TM + TN; ++i) read(smem, i, 0);
-
-  // the stages of slab i and of slab i + 1 (an even number of slabs in all)
-  char *st = smem, *next = smem + STAGE;
-  for (int base = 0; base < nslab; base += 2) {
+  for (int d = 0; d < D; ++d) fetch(d, d);
+  wait(std::integral_constant<int, (NX - 2) * PX + D * TN>{});
+  char *xs = smem, *xfree = smem + (NX - 1) * XS;  // this slab's stage, and the one before it
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      // slab i + 1 has landed for every wave, and every wave has read slab i
-      wait(std::integral_constant<int, (NS - 2) * PER>{});
-      issue(base + b + NS, st);
-      constexpr int NMF = TM * TN, NR = TM + TN, EVERY = NMF / NR > 0 ? NMF / NR : 1;
-      int r = 0;
+  for (int i = 0; i < LA; ++i) fx[i] = *(const i32x4*)(xs + xr + xc[0] + i * 2048);
+  int slab = 0;
+  for (int own = 0; own < KS / KG; own += D) {
 #pragma unroll
-      for (int x = 0; x < NMF; ++x) {
-        if (x % EVERY == 0 && r < NR) read(next, r++, b ^ 1);
-        const int n = x / TM, m = x % TM;
-        acc[n][m] = mfma_i8(fw[b][n], fx[b][m], acc[n][m]);
-        __builtin_amdgcn_sched_barrier(0x406);
+    for (int d = 0; d < D; ++d) {
+      constexpr int LAST = SP - 1;
+      const int p = d % SP;
+      const char* xnext = xs;
+      if (p == LAST) {
+        // the next slab of x has landed (behind it came NX - 3 slabs and W of NX - 2 slabs' steps), and the one before
+        // this has been read by all
+        wait(std::integral_constant<int, (NX - 3) * PX + (D < (NX - 2) * SP ? D : (NX - 2) * SP) * TN>{});
+        xnext = xs == smem + (NX - 1) * XS ? smem : xs + XS;
+        issue_x(slab + NX - 1, xfree);
       }
 #pragma unroll
-      for (; r < NR; ++r) read(next, r, b ^ 1);
-      st = next;
-      next = next == smem + (NS - 1) * STAGE ? smem : next + STAGE;
+      for (int m = 0; m < TM; ++m) {
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+          acc[n][m] = mfma_i8(w[d][n], fx[m % LA], acc[n][m]);
+          __builtin_amdgcn_sched_barrier(0x406);
+        }
+        const int f = m + LA;
+        fx[m % LA] = *(const i32x4*)((f < TM ? xs : xnext) + xr + xc[f < TM ? p : (p + 1) % SP] + f % TM * 2048);
+        __builtin_amdgcn_sched_barrier(0x406);
+      }
+      fetch(own + d + D, d);
+      if (p == LAST) {
+        xfree = xs;
+        xs = (char*)xnext;
+        ++slab;
+      }
     }
   }
-  __builtin_amdgcn_s_waitcnt(0x0070);  // nothing of this workgroup's on its way into LDS
+  __builtin_amdgcn_s_waitcnt(0x0070);  // nothing of this workgroup's is on its way into LDS
 
   if constexpr (KG > 1) {
     __syncthreads();
-    i32x4* red = (i32x4*)smem + (wm * WGN + wn) * TM * TN * 64 + lane;
+    i32x4* red = (i32x4*)smem + wn * TM * TN * 64 + lane;
     if (kg == 1) {
 #pragma unroll
       for (int n = 0; n < TN; ++n)
@@ -356,18 +356,18 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG) void w8_tile_kernel(GemmI8Args
     // a row at a time: its residuals are all asked for before its results are stored
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
-      const int row = wm * WM + m * 16 + c16;
+      const int row = m * 16 + c16;
       const bool in = row < rows;
       const float sx = a.sx[m0 + min(row, rows - 1)];
       const uint32_t at = row * (uint32_t)a.ldo;
       f32x4 y[TO];
 #pragma unroll
       for (int n = 0; n < TO; ++n) {
-        const i32x4 v = acc[SWIGLU ? n / 2 * 4 + n % 2 : n][m];
+        const i32x4 v = acc[SWIGLU ? 2 * n : n][m];
 #pragma unroll
         for (int x = 0; x < 4; ++x) y[n][x] = (float)v[x] * sx * ws[n][x];
         if constexpr (SWIGLU) {
-          const i32x4 u = acc[n / 2 * 4 + 2 + n % 2][m];
+          const i32x4 u = acc[2 * n + 1][m];
 #pragma unroll
           for (int x = 0; x < 4; ++x) y[n][x] = silu_of(y[n][x]) * ((float)u[x] * sx * us[n][x]);
         }
@@ -388,29 +388,77 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG) void w8_tile_kernel(GemmI8Args
   });
 }
 
-template <int BM, int BN, int WGM, int WGN, int KG, int NS>
+template <int BM, int BN, int WGN, int KG, int NX, int D, int LA>
 hipError_t launch_tile(const GemmI8Args& a, hipStream_t s) {
   const int64_t wgs = ((int64_t)a.M + BM - 1) / BM * ((a.N + BN - 1) / BN);
-  if (wgs >= (1ll << 32) / (64 * WGM * WGN * KG)) return hipErrorInvalidValue;  // threads of a launch
-  const dim3 grid((unsigned)wgs), block(64 * WGM * WGN * KG);
-  if (a.swiglu)
-    hipLaunchKernelGGL((w8_tile_kernel<BM, BN, WGM, WGN, KG, NS, true>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((w8_tile_kernel<BM, BN, WGM, WGN, KG, NS, false>), grid, block, 0, s, a);
+  if (wgs >= (1ll << 32) / (64 * WGN * KG)) return hipErrorInvalidValue;  // threads of a launch
+  const dim3 grid((unsigned)wgs), block(64 * WGN * KG);
+  if (a.swiglu) {
+    if constexpr (BN / WGN % 32 == 0)
+      hipLaunchKernelGGL((w8_tile_kernel<BM, BN, WGN, KG, NX, D, LA, true>), grid, block, 0, s, a);
+    else
+      return hipErrorInvalidValue;
+  } else {
+    hipLaunchKernelGGL((w8_tile_kernel<BM, BN, WGN, KG, NX, D, LA, false>), grid, block, 0, s, a);
+  }
   return hipGetLastError();
 }
-template <int NT, int MT, int W, int U>
+template <int NT, int W, int U>
 hipError_t launch_rows(const GemmI8Args& a, hipStream_t s) {
-  const int tiles = a.swiglu ? tiles_of(a.N) / 2 : (a.N + 15) / 16, tw = a.swiglu ? NT / 2 : NT;
-  const dim3 grid(cdiv(tiles, tw), cdiv(a.M, 16 * MT)), block(W * 64);
+  const dim3 grid(cdiv(a.swiglu ? tiles_of(a.N) / 2 : tiles_of(a.N), a.swiglu ? NT / 2 : NT)), block(W * 64);
   if constexpr (NT > 1) {
     if (a.swiglu) {
-      hipLaunchKernelGGL((w8_rows_kernel<NT, MT, W, U, true>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((w8_rows_kernel<NT, W, U, true>), grid, block, 0, s, a);
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((w8_rows_kernel<NT, MT, W, U, false>), grid, block, 0, s, a);
+  hipLaunchKernelGGL((w8_rows_kernel<NT, W, U, false>), grid, block, 0, s, a);
   return hipGetLastError();
+}
+
+// The tile of a product over more than 16 rows: the one whose estimated time is least.
+// Workgroups run in rounds of 256 per_cu; a workgroup takes t us for a slab of 128 k and f us
+// for its ends, and t grows with the number that run together, since they share L2 and,
+// past 256, a CU: t0 for few, t1 for one on every CU, step more as the first CUs take a
+// second one, t2 for two on every CU, t3 for three.  The figures are a least-squares fit to 7000
+// products timed in every tile with their weights read from memory (M = 17 to 4096, N =
+// 256 to 22016, K = 256 to 11008; mean error 9 to 13%); what the choice takes is
+// 1.8% slower than the fastest tile on average, 23% in one of a hundred, 39% at most.  us,
+// the same four products in each tile (- : not timed):
+//                                        128x512 128x256 64x256 128x128 64x128 48x128 64x64 32x64 32x32
+//   2048 x 22016, K =  4096, gated            161     167    218     191    261      -   286     -     -
+//   2048 x 12288, K =  4096                   110      91    123     107    146      -   163     -     -
+//    333 x  4096, K = 11008, residual         115      68     56      48     35     36    42    50    60
+//     64 x  4096, K = 11008, residual          95      53     40      33     28     24    20    15    14 (from cache)
+struct Tile {
+  int rows, cols, per_cu;
+  float t0, t1, step, t2, t3, f;
+};
+constexpr Tile kTiles[] = {
+    {128, 512, 1, 0.984f, 1.819f, 0.f, 0.f, 0.f, 9.08f},        {128, 256, 1, 0.546f, 0.950f, 0.f, 0.f, 0.f, 5.49f},
+    {64, 256, 2, 0.390f, 0.767f, 0.432f, 1.276f, 0.f, 3.61f},   {128, 128, 2, 0.335f, 0.689f, 0.432f, 1.130f, 0.f, 5.90f},
+    {64, 128, 2, 0.248f, 0.461f, 0.351f, 0.728f, 0.f, 3.83f},   {48, 128, 2, 0.216f, 0.440f, 0.344f, 0.673f, 0.f, 3.25f},
+    {64, 64, 3, 0.158f, 0.270f, 0.135f, 0.660f, 0.674f, 3.54f}, {32, 64, 3, 0.115f, 0.197f, 0.125f, 0.480f, 0.465f, 2.48f},
+    {32, 32, 3, 0.079f, 0.115f, 0.074f, 0.338f, 0.278f, 2.67f}};
+constexpr int kTileCount = sizeof(kTiles) / sizeof(kTiles[0]);
+int choose_tile(int M, int N, int K) {
+  const float slabs = (float)(steps_of(K) / 2);
+  int best = 0;
+  float least = 0.f;
+  for (int i = 0; i < kTileCount; ++i) {
+    const Tile& t = kTiles[i];
+    const int64_t wgs = ((int64_t)M + t.rows - 1) / t.rows * (((int64_t)N + t.cols - 1) / t.cols), round = 256 * t.per_cu;
+    auto slab_us = [&](int64_t n) {
+      const float x = (float)n / 256.f;
+      return x <= 1.f   ? t.t0 + (t.t1 - t.t0) * x
+             : x <= 2.f ? t.t1 + t.step + (t.t2 - t.t1 - t.step) * (x - 1.f)
+                        : t.t2 + (t.t3 - t.t2) * (x - 2.f);
+    };
+    float us = (float)(wgs / round) * (slab_us(round) * slabs + t.f);
+    if (wgs % round) us += slab_us(wgs % round) * slabs + t.f;
+    if (i == 0 || us < least) least = us, best = i;
+  }
+  return best;
 }
 
 // One thread per 16 bytes of the packed codes, then the scales.
@@ -444,10 +492,33 @@ hipError_t w8_pack(const int8_t* codes, const float* scales, void* wp, int N, in
   return hipGetLastError();
 }
 
+void gemm_i8_tile(int M, int N, int K, int* rows, int* cols) {
+  const Tile t = M > 16 ? kTiles[choose_tile(M, N, K)] : Tile{};
+  *rows = t.rows;
+  *cols = t.cols;
+}
+
 hipError_t gemm_i8(const GemmI8Args& a, hipStream_t s) {
-  if (a.M <= 16) return launch_rows<2, 1, 8, 4>(a, s);
-  if ((int64_t)a.M * a.N >= 256ll * 256 * 200) return launch_tile<256, 256, 2, 4, 1, 4>(a, s);
-  return launch_tile<128, 128, 2, 2, 1, 4>(a, s);
+  if (a.M <= 16) {
+    // waves and tiles a workgroup by the number of tiles.  us, one row, weights from memory, 8 waves, 4 waves, 4 waves
+    // of two tiles: N = 4096, K = 4096 5.7, 6.2, 7.2; N = 12288 11.4, 11.1, 12.1; 16 rows, N = 57344, K = 8192 110, 107, and 90
+    // as 8 waves of two tiles
+    if (a.swiglu) return launch_rows<2, 8, 2>(a, s);
+    return a.N <= 8192    ? launch_rows<1, 8, 4>(a, s)
+           : a.N <= 16384 ? launch_rows<1, 4, 4>(a, s)
+                          : launch_rows<2, 8, 2>(a, s);
+  }
+  switch (choose_tile(a.M, a.N, a.K)) {  // the table's order
+    case 0: return launch_tile<128, 512, 8, 1, 3, 4, 4>(a, s);
+    case 1: return launch_tile<128, 256, 8, 1, 4, 4, 4>(a, s);
+    case 2: return launch_tile<64, 256, 8, 1, 4, 4, 4>(a, s);
+    case 3: return launch_tile<128, 128, 4, 2, 4, 4, 4>(a, s);
+    case 4: return launch_tile<64, 128, 4, 2, 4, 4, 4>(a, s);
+    case 5: return launch_tile<48, 128, 4, 2, 6, 4, 3>(a, s);
+    case 6: return launch_tile<64, 64, 2, 2, 6, 4, 4>(a, s);
+    case 7: return launch_tile<32, 64, 2, 2, 6, 4, 2>(a, s);
+    default: return launch_tile<32, 32, 1, 2, 8, 8, 2>(a, s);
+  }
 }
 
 }  // namespace vla

@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+from i8_tiles import TILES
 from paper_2608_14586_amd import binding as vb
 
 pytestmark = pytest.mark.gpu
@@ -182,6 +183,19 @@ def test_gemm_i8(M, N, K):
 def test_gemm_i8_gated(M, N, K):
     _product(M, N, K, "swiglu", wide=8)
     _product(M, N, K, "swiglu")
+
+
+@pytest.mark.parametrize("tile", list(TILES))
+def test_gemm_i8_tiles(tile):
+    """Every tile at odd sizes, each output, aligned rows of outputs and others."""
+    for M, N, K, gated in TILES[tile]:
+        assert vb.vla_op_gemm_i8_tile(M, N, K) == tile
+        if gated:
+            _product(M, N, K, "swiglu")
+            _product(M, N, K, "swiglu", seed=1, wide=3)
+        else:
+            for i, out in enumerate(("bf16", "f32", "add")):
+                _product(M, N, K, out, seed=i, wide=i + 3)
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 12288, 4096), (333, 4096, 2048), (2048, 2048, 512), (3000, 5000, 128), (700, 9000, 256), (1500, 2500, 384), (5, 100, 131056)])

@@ -76,3 +76,16 @@ def test_binding_refuses_before_the_library():
                  lambda: vb.vla_op_w8_pack(x, s, Wp), lambda: vb.vla_op_w8_pack(None, s, Wp)):
         with pytest.raises(ValueError):
             call()
+
+
+
+def test_tiles():
+    """The shapes that the GPU tests run in every tile do take it."""
+    from i8_tiles import TILES
+    assert len(TILES) == 10
+    for tile, shapes in TILES.items():
+        for M, N, K, gated in shapes:
+            assert vb.vla_op_gemm_i8_tile(M, N, K) == tile and (not gated or N % 64 == 0)
+    for bad in ((0, 64, 64), (-1, 64, 64), (20, 0, 64), (20, 64, 24)):
+        with pytest.raises(vb.VlaError):
+            vb.vla_op_gemm_i8_tile(*bad)
