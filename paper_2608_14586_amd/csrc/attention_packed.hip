@@ -3,8 +3,8 @@
 //   o_t = sum_{j <= t} exp(q_t k_j / sqrt(dh) - m_t) v_j / sum_{j <= t} exp(...)   within a prompt
 //
 // Bound by the matrix cores: 4 dh operations a pair of a query and a key that it sees.
-// One workgroup of 4 waves takes 128 NQ queries of a prompt and head, a wave 32 NQ of
-// them side by side.  Keys advance in tiles of 64 that all waves share, K and V as they
+// One workgroup of 4 waves takes 128 queries of a prompt and head, a wave 32 of them
+// side by side.  Keys advance in tiles of 64 that all waves share, K and V as they
 // lie in memory, rows of dh, moved by buffer_load ... lds into two stages; rows past the
 // prompt's end read as zero through the buffer, whatever lies there.
 //
@@ -17,14 +17,23 @@
 // two a v_dot2, so weights and sum are rounded alike.
 //
 // A wave works one tile ahead: between the exponentials of tile t its MFMAs form the
-// scores of tile t + 1.  With NQ = 2 every operand that is read from LDS serves two
-// MFMAs.  At NQ = 1 LDS, 128 bytes a cycle, is as busy as the matrix cores: 1 KB a
-// 32-cycle MFMA on each of 4 SIMDs.
+// scores of tile t + 1.  One long prompt (16384 tokens, 8 heads of 128) takes 520 us, 1060
+// TF/s of the half that is not masked: the matrix cores are busy for 62% of the cycles, at
+// the 1.6 GHz that the chip holds under it.  Four prompts of 4096, 2048, 1201 and 847, 32 heads:
+// 202 to 225 us.  With less to do a tile takes a workgroup that has a CU alone 1.05 us, its
+// parts one behind the other: without the loads 0.93, without exponentials 1.0, without
+// three quarters of the PV products 1.0.  What did not help: 64 queries a wave (half the LDS reads,
+// but 268 us for 225: accumulators wander between the register files), the next tile's maximum and
+// half of its weights between the PV products (16384 tokens 4% faster, prompts of 2048 4%
+// slower), a third stage of values (0 to 10% slower), and key tiles dealt out to two groups of four
+// waves (10 to 18% faster where fewer than 256 workgroups have 15 tiles and more, else slower;
+// and a prompt's bits would depend on the others of the call).
 //
-// Only a wave's last tile has masked keys, and there only one half of 32 keys a set of 32
-// queries.  A value there that is not finite must not reach the queries that do not see it
-// (0 NaN is NaN): they are looked for, and where there is one (rarely) such values are
-// taken as 0 and a product of (not finite) with (sees it) marks what they make NaN.
+// Only a wave's last tile has masked keys, in one half of its 64 (the other is seen by all of
+// the wave's queries, or by none).  A value there that is not finite must not reach the
+// queries that do not see it (0 NaN is NaN): such are looked for, and where there is one
+// (rarely) they are taken as 0, and a product of (not finite) with (sees it) marks what they
+// make NaN.
 //
 // Workgroups take tiles of queries longest first (found from the offsets by each one), all
 // heads of a tile side by side.
@@ -52,35 +61,60 @@ __device__ __forceinline__ void landed() {
   asm volatile("" ::: "memory");
 }
 
+// over the wave, without a trip through LDS for each step
+template <int CTRL>
+__device__ __forceinline__ int dpp_i(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true);
+}
 __device__ __forceinline__ int wave_sum_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return __builtin_amdgcn_readfirstlane(v);
+  v += dpp_i<0xB1>(v);
+  v += dpp_i<0x4E>(v);
+  v += dpp_i<0x141>(v);
+  v += dpp_i<0x140>(v);
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) +
+         __builtin_amdgcn_readlane(v, 48);
 }
 
-// Tile number `id` of the call's, in tiles of BQ queries: prompt rows [start, start +
-// len), queries from q0 on; len = 0 where there is no such tile.  Up to 64 prompts, tiles
-// come in the order of their lengths: tile number n of a prompt has n + 1 tiles' work, and
-// F(n) = sum over prompts of max(tiles - n, 0) tiles have number n or more.  More prompts:
-// one behind the other.
+// The tile of BQ queries and the head (of H, some order) of workgroup `wg`: prompt rows
+// [start, start + len), queries from q0 on; len = 0 where there is no such tile.  Up to 64
+// prompts, tiles come longest first, all heads of one side by side: tile number n of a
+// prompt has n + 1 tiles' work, and F(n) = sum over prompts of max(tiles - n, 0) tiles have
+// number n or more.  Where all workgroups run at once, workgroup i and i + 256 on one CU, a
+// CU's two are a long and a short one, and the longest have a CU alone (32 heads of 128, one
+// prompt of 2048: 47 us, in plain order 49).  More prompts: one behind the other.
 struct Work {
-  int start, len, q0;
+  int start, len, q0, head;
 };
-__device__ __forceinline__ Work work_of(const int32_t* offsets, int n_seq, int T, int id, int BQ) {
+__device__ __forceinline__ Work work_of(const PackedAttn& p, int wg, int BQ) {
+  const int32_t* offsets = p.offsets;
+  const int n_seq = p.n_seq, T = p.T, H = p.H;
   const int lane = threadIdx.x & 63;
-  auto lane_seq = [&](int first, int& start, int& len) {
-    const int i = first + lane;
+  auto lane_seq = [&](int from, int& start, int& len) {
+    const int i = from + lane;
     const int a = i < n_seq ? offsets[i] : 0, b = i < n_seq ? offsets[i + 1] : 0;
     start = min(max(a, 0), T);
     len = max(min(max(b, 0), T) - start, 0);
     return (len + BQ - 1) / BQ;
   };
-  Work w{0, 0, 0};
-  int start, len, nt, pick = -1, tile = 0;
+  Work w{0, 0, 0, 0};
+  int start, len, nt, pick = -1, tile = 0, id;
   if (n_seq <= 64) {
     nt = lane_seq(0, start, len);
+    const int total = wave_sum_i(nt), all = total * H;  // the launch has at least as many, below 2^24
+    int rank = wg;
+    if (all > 256 && all <= 512) {
+      const int twice = all - 256;  // CUs with two
+      if (wg < 256) {
+        rank = wg < twice ? 256 - twice + wg : wg - twice;
+      } else {  // whole tiles from the shortest on, then what the first 256 left of theirs
+        const int e = wg - 256, whole = (total - 1 - div_by(256, p.by_H)) * H, t = div_by(e, p.by_H);
+        rank = e < whole ? (total - 1 - t) * H + e - t * H : 256 + e - whole;
+      }
+    }
+    id = div_by(rank, p.by_H);
+    w.head = rank - id * H;
+    if (total <= id) return w;
     int lo = 0, hi = (T + BQ - 1) / BQ, more = 0;  // F(lo) > id >= F(hi) = more
-    if (wave_sum_i(nt) <= id) return w;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2, f = wave_sum_i(max(nt - mid, 0));
       if (f > id)
@@ -93,9 +127,11 @@ __device__ __forceinline__ Work work_of(const int32_t* offsets, int n_seq, int T
     pick = __builtin_ctzll(has);
     tile = lo;
   } else {
+    id = div_by(wg, p.by_H);
+    w.head = wg - id * H;
     int before = 0;
-    for (int first = 0; first < n_seq; first += 64) {
-      nt = lane_seq(first, start, len);
+    for (int from = 0; from < n_seq; from += 64) {
+      nt = lane_seq(from, start, len);
       int upto = nt;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -118,11 +154,11 @@ __device__ __forceinline__ Work work_of(const int32_t* offsets, int n_seq, int T
   return w;
 }
 
-template <int DH, int NQ>
-__global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention_packed_kernel(PackedAttn a) {
+template <int DH>
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attention_packed_kernel(PackedAttn a) {
   constexpr int ROWB = DH * 2, TILE = BKV * ROWB, LOADS = TILE / 1024 / 4;  // 1 KB loads a wave and tile of K or V
   constexpr int RPK = 1024 / ROWB, CPR = ROWB / 16;                         // rows a load, 16-byte chunks a row
-  constexpr int ND = DH / 32, KS = DH / 16, BQ = 128 * NQ;
+  constexpr int ND = DH / 32, KS = DH / 16, BQ = 128;
   // one array per operand and stage: the compiler can tell reads from the loads into other arrays
   __shared__ __attribute__((aligned(1024))) char sk0[TILE];
   __shared__ __attribute__((aligned(1024))) char sk1[TILE];
@@ -131,26 +167,25 @@ __global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, li = lane & 31;
-  const int ti = div_by(blockIdx.x, a.by_H), hr = blockIdx.x - ti * a.H;
-  // heads of a KV head H / Hkv ids apart ... 8 ids side by side go to 8 XCDs
-  const int gi = div_by(hr, a.by_Hkv), hk = hr - gi * a.Hkv, h = hk * a.G + gi;
-  const Work wk = work_of(a.offsets, a.n_seq, a.T, ti, BQ);
+  const Work wk = work_of(a, blockIdx.x, BQ);
   if (wk.len == 0) return;
-  const int L = wk.len, q0 = wk.q0, qw0 = q0 + wave * 32 * NQ;
+  // 8 heads side by side go to the 8 XCDs, each with a KV head's own queries where there are 8 KV heads
+  const int gi = div_by(wk.head, a.by_Hkv), hk = wk.head - gi * a.Hkv, h = hk * a.G + gi;
+  const int L = wk.len, q0 = wk.q0, qw0 = q0 + wave * 32;
 
   const bf16_t* kh = (const bf16_t*)a.k.p + (int64_t)wk.start * a.k.token + hk * a.k.head;
   const bf16_t* vh = (const bf16_t*)a.v.p + (int64_t)wk.start * a.v.token + hk * a.v.head;
 
   // the wave's queries as MFMA B operands; lanes past L load row L - 1 (not stored)
-  bf16x8 fq[NQ][KS];
+  const int qi = qw0 + li;
+  bf16x8 fq[KS];
+  {
+    const bf16_t* row = (const bf16_t*)a.q.p + (int64_t)(wk.start + min(qi, L - 1)) * a.q.token + h * a.q.head;
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const bf16_t* row = (const bf16_t*)a.q.p + (int64_t)(wk.start + min(qw0 + n * 32 + li, L - 1)) * a.q.token + h * a.q.head;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) fq[n][ks] = *(const bf16x8*)(row + ks * 16 + half * 8);
+    for (int ks = 0; ks < KS; ++ks) fq[ks] = *(const bf16x8*)(row + ks * 16 + half * 8);
   }
   const int ntiles = (min(L, q0 + BQ) + BKV - 1) / BKV;
-  const int mine = min(qw0, L - 1) / BKV;  // the wave's last tile; waves without queries follow the last one that has
+  const int full = qw0 / BKV;  // tiles that the wave's queries see whole; the next one is its last
   const bool work = qw0 < L;
 
   // K row r: chunk c stored at c ^ ksw(r), so that 32 rows of one chunk meet every bank alike; V row r: at c ^ vsw(r), so
@@ -185,23 +220,19 @@ __global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention
     for (int j = 0; j < LOADS; ++j) dma16(r, st + (wave * LOADS + j) * 1024, vv, (int)(j * RPK * a.v.token * 2));
   };
 
-  f32x16 acc[NQ][ND];
+  f32x16 acc[ND];
 #pragma unroll
-  for (int n = 0; n < NQ; ++n)
+  for (int t = 0; t < ND; ++t)
 #pragma unroll
-    for (int t = 0; t < ND; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[n][t][r] = 0.f;
-  float m[NQ], l[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) m[n] = -INFINITY, l[n] = 0.f;
+    for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
 
   // K tile t + 2 and V tile t + 1 go out at the head of tile t, into the stages that tile t - 1 read last
   issue_k(sk0, 0);
   issue_k(sk1, 1);
   issue_v(sv0, 0);
 
-  f32x16 sa[NQ][2], sb[NQ][2];  // scores of the tile in work and of the next
+  f32x16 sa[2], sb[2];  // scores of the tile in work and of the next
   const f32x16 zero = {};
   auto kfrag = [&](const char* st, int t, int ks) -> bf16x8 {
     const int r = t * 32 + li, c = ks * 2 + half;
@@ -225,38 +256,35 @@ __global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const bf16x8 f = kfrag(sk0, t, ks);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-          sa[n][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, fq[n][ks], ks == 0 ? zero : sa[n][t], 0, 0, 0);
+        sa[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(sk0, t, ks), fq[ks], ks == 0 ? zero : sa[t], 0, 0, 0);
       }
   }
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f}, none = {(__bf16)0.f, (__bf16)0.f};
 
-  // the maximum of a set's scores; moves the running one where a score is 8 (in log2) above it
-  auto raise = [&](int n, const f32x16(&s)[2]) {
+  // the running maximum moves where a score is 8 (in log2) above it
+  auto raise = [&](const f32x16(&s)[2]) {
     float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
-    if (__any(top > m[n] + 8.f)) {
+    if (__any(top > m + 8.f)) {
       // by the query's own scores alone: its bits do not depend on its neighbours
-      const float mn = top > m[n] + 8.f ? top : m[n], f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mn);
-      l[n] *= f;
+      const float mn = top > m + 8.f ? top : m, f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= f;
 #pragma unroll
       for (int t = 0; t < ND; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[n][t][r] *= f;
-      m[n] = mn;
+        for (int r = 0; r < 16; ++r) acc[t][r] *= f;
+      m = mn;
     }
   };
-  // weights x, x + 1 of a set (x = 16 t + r) as a bf16 pair, added to its sum
-  auto weigh = [&](int n, const f32x16(&s)[2], int x) {
-    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][x & 15], a.scale_log2, -m[n]));
-    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][(x & 15) + 1], a.scale_log2, -m[n]));
+  // weights x, x + 1 (x = 16 t + r) as a bf16 pair, added to the sum
+  auto weigh = [&](const f32x16(&s)[2], int x) {
+    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][x & 15], a.scale_log2, -m));
+    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][(x & 15) + 1], a.scale_log2, -m));
     const bf16x2 w = {(__bf16)p0, (__bf16)p1};
-    l[n] = __builtin_amdgcn_fdot2_f32_bf16(w, ones, l[n], false);
+    l = __builtin_amdgcn_fdot2_f32_bf16(w, ones, l, false);
     return __builtin_bit_cast(uint32_t, w);
   };
   auto operand = [](const uint32_t* p) { return __builtin_bit_cast(bf16x8, u32x4{p[0], p[1], p[2], p[3]}); };
@@ -297,7 +325,7 @@ __global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention
   };
 
   // tile it in stage S (= it % 2): s holds its scores, sn receives the next tile's
-  auto body = [&](auto S_, int it, f32x16(&s)[NQ][2], f32x16(&sn)[NQ][2]) {
+  auto body = [&](auto S_, int it, f32x16(&s)[2], f32x16(&sn)[2]) {
     constexpr int S = decltype(S_)::value;
     // K tile it + 1 and V tile it landed, and every wave is done with the stages that the next loads overwrite
     landed();
@@ -307,74 +335,61 @@ __global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention
       issue_k(S == 0 ? sk0 : sk1, it + 2);
       issue_v(S == 0 ? sv1 : sv0, it + 1);
     }
-    if (work && it < mine) {
-      uint32_t p[NQ][16];
+    if (work && it < full) {
+      uint32_t p[16];
       // operands in order: the next tile's K (NK), then this tile's V; read LA ahead of the MFMAs that take them.
       // The scheduling barriers let only VALU and scalar instructions cross, so this order is the one issued.
-      constexpr int NK = 2 * KS, NV = 4 * ND, LA = 4, PPK = 16 / NK > 0 ? 16 / NK : 1;
+      constexpr int NK = 2 * KS, NP = 4 * ND, LA = 4;
       bf16x8 fr[LA];
       auto fetch = [&](int i) {
         if (i < NK)
           fr[i % LA] = kfrag(kst, i & 1, i >> 1);
-        else if (i < NK + NV)
+        else if (i < NK + NP)
           fr[i % LA] = vfrag(vst, (i - NK) / ND, (i - NK) % ND);
       };
 #pragma unroll
       for (int i = 0; i < LA; ++i) fetch(i);
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) raise(n, s[n]);
+      raise(s);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         const int ks = i >> 1, t = i & 1;
+        sn[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % LA], fq[ks], ks == 0 ? zero : sn[t], 0, 0, 0);
+        fetch(i + LA);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          sn[n][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % LA], fq[n][ks], ks == 0 ? zero : sn[n][t], 0, 0, 0);
-          if (n == NQ - 1) fetch(i + LA);
-#pragma unroll
-          for (int x = i * PPK; x < (i + 1) * PPK; ++x) p[n][x] = weigh(n, s[n], 2 * x);
-          __builtin_amdgcn_sched_barrier(0x406);
-        }
+        for (int x = i * 16 / NK; x < (i + 1) * 16 / NK; ++x) p[x] = weigh(s, 2 * x);
+        __builtin_amdgcn_sched_barrier(0x406);
       }
 #pragma unroll
-      for (int c4 = 0; c4 < 4; ++c4)
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-          const int i = NK + c4 * ND + dt;
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            acc[n][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % LA], operand(p[n] + 4 * c4), acc[n][dt], 0, 0, 0);
-            if (n == NQ - 1) fetch(i + LA);
-            __builtin_amdgcn_sched_barrier(0x406);
-          }
-        }
+      for (int j = 0; j < NP; ++j) {
+        acc[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[(NK + j) % LA], operand(p + 4 * (j / ND)), acc[j % ND], 0, 0, 0);
+        fetch(NK + j + LA);
+        __builtin_amdgcn_sched_barrier(0x406);
+      }
     }
   };
   for (int base = 0; base < ntiles; base += 2) {
     body(std::integral_constant<int, 0>{}, base, sa, sb);
     if (base + 1 < ntiles) body(std::integral_constant<int, 1>{}, base + 1, sb, sa);
   }
+  // The wave's last tile: of its two halves of 32 keys, `diag` up to the query's own, the one before it whole, none
+  // after.  The last two tiles' values are both still there.
   if (!work) return;
-  // the last two tiles' values are both still there
-  char* const vst = mine & 1 ? sv1 : sv0;
-  if (mine & 1)
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) sa[n][0] = sb[n][0], sa[n][1] = sb[n][1];
-  // the wave's last tile: of a set, the keys of half `diag` up to its own, those of the half before it, none after
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const int diag = NQ == 2 ? n : wave & 1;
+  {
+    char* const vst = full & 1 ? sv1 : sv0;
+    if (full & 1) sa[0] = sb[0], sa[1] = sb[1];
+    const int diag = wave & 1;
     uint32_t p[16];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int key = t * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-        sa[n][t][r] = key <= diag * 32 + li ? sa[n][t][r] : -INFINITY;
+        sa[t][r] = key <= diag * 32 + li ? sa[t][r] : -INFINITY;
       }
-    raise(n, sa[n]);
+    raise(sa);
 #pragma unroll
-    for (int x = 0; x < 16; ++x) p[x] = weigh(n, sa[n], 2 * x);
+    for (int x = 0; x < 16; ++x) p[x] = weigh(sa, 2 * x);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if (t > diag) break;
@@ -391,42 +406,38 @@ __global__ __launch_bounds__(256, NQ == 2 ? 1 : DH == 64 ? 3 : 2) void attention
           if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
         dirty = __any(bad != bad);
-        if (dirty) mark(acc[n], vst, t);
+        if (dirty) mark(acc, vst, t);
       }
 #pragma unroll
       for (int i = 0; i < 2 * ND; ++i) {
         bf16x8 f = vfrag(vst, 2 * t + i / ND, i % ND);
         if (dirty) f = without(f, nullptr);
-        acc[n][i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, operand(p + 4 * (2 * t + i / ND)), acc[n][i % ND], 0, 0, 0);
+        acc[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, operand(p + 4 * (2 * t + i / ND)), acc[i % ND], 0, 0, 0);
         if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
 
+  const float total = l + __shfl_xor(l, 32, 64);
+  if (qi < L) {
+    const float inv = 1.f / total;
+    bf16_t* row = (bf16_t*)a.o.p + (int64_t)(wk.start + qi) * a.o.token + h * a.o.head;
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const float total = l[n] + __shfl_xor(l[n], 32, 64);
-    const int qi = qw0 + n * 32 + li;
-    if (qi < L) {
-      const float inv = 1.f / total;
-      bf16_t* row = (bf16_t*)a.o.p + (int64_t)(wk.start + qi) * a.o.token + h * a.o.head;
+    for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *(u32x2*)(row + dt * 32 + g * 8 + half * 4) =
-              u32x2{pack_bf2(acc[n][dt][g * 4 + 0] * inv, acc[n][dt][g * 4 + 1] * inv),
-                    pack_bf2(acc[n][dt][g * 4 + 2] * inv, acc[n][dt][g * 4 + 3] * inv)};
-    }
+      for (int g = 0; g < 4; ++g)
+        *(u32x2*)(row + dt * 32 + g * 8 + half * 4) =
+            u32x2{pack_bf2(acc[dt][g * 4 + 0] * inv, acc[dt][g * 4 + 1] * inv),
+                  pack_bf2(acc[dt][g * 4 + 2] * inv, acc[dt][g * 4 + 3] * inv)};
   }
 }
 
-template <int DH, int NQ>
+template <int DH>
 hipError_t launch(const PackedAttn& a, hipStream_t s) {
-  // every tile but a prompt's last has 128 NQ queries
-  const int64_t tiles = (int64_t)a.T / (128 * NQ) + a.n_seq, wgs = tiles * a.H;
+  // every tile but a prompt's last has 128 queries
+  const int64_t wgs = ((int64_t)a.T / 128 + a.n_seq) * a.H;
   if (wgs >= 1ll << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
-  hipLaunchKernelGGL((attention_packed_kernel<DH, NQ>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attention_packed_kernel<DH>), dim3((unsigned)wgs), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -437,7 +448,7 @@ hipError_t attention_packed(PackedAttn a, int dh, hipStream_t s) {
   a.by_H = fast_div(a.H);
   a.by_Hkv = fast_div(a.Hkv);
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
-  return dh == 128 ? launch<128, 1>(a, s) : launch<64, 1>(a, s);
+  return dh == 128 ? launch<128>(a, s) : launch<64>(a, s);
 }
 
 }  // namespace vla
