@@ -276,7 +276,10 @@ using Kv8Rows = Kv4Rows;
 size_t kv8_bytes(int B, int Hkv, int L_cap, int dh);
 hipError_t kv8_store(Kv8Rows a, int dh, hipStream_t s);
 hipError_t kv8_load(Kv8Rows a, int dh, hipStream_t s);
-using Kv8Attn = Kv4Attn;
+struct Kv8Attn : Kv4Attn {
+  int tiles;  // of query rows, a KV head
+  FastDiv by_BH, by_tiles;
+};
 size_t kv8_attention_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
 // hipErrorOutOfMemory: a.part is smaller than kv8_attention_scratch
 hipError_t kv8_attention(Kv8Attn a, int dh, size_t scratch_bytes, hipStream_t s);

@@ -80,7 +80,10 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
 // One workgroup for the keys of a block (even ones) or for its values.  Every thread
 // quantises a piece of a row, the codes cross LDS, and every thread writes 16 bytes of
 // the block as it lies in memory, with the codes of positions that the call does not
-// store as they were (or rescaled, where the block's exponent grows).
+// store as they were (or rescaled, where the block's exponent grows).  Memory bounds it:
+// 2048 tokens of 32 heads of 128, 50 MB in all, take 13.1 us (3.8 TB/s, the launch's 2.3 us
+// included), a token of each of four sequences of two heads 3.3.  Values transposed in
+// registers and all rows in whole cache lines through LDS measured 13.2 us.
 template <int DH>
 __global__ __launch_bounds__(2 * DH) void kv8_store_kernel(Kv8Rows a) {
   constexpr int T = 2 * DH, W = T / 64, TPR = T / BLK, V = DH / TPR;  // threads a row, values a thread: 16
@@ -190,13 +193,49 @@ __global__ __launch_bounds__(2 * DH) void kv8_store_kernel(Kv8Rows a) {
   if (tid == 0) *step = now;
 }
 
-// The inverse, keys from memory as they lie, values through LDS.
+// A block lies in memory as 16 bytes for each thread, of keys those of token 16 t + lane % 16, dims d .. d + 7 and
+// d + 32 .. d + 39.  For rows written in whole cache lines they cross LDS: thread tid's part
+// of the keys is dims d .. d + 7 of token t and of token t + 16, two words of four codes each.  The pieces of 64 lanes
+// lie 16 bytes further apart than in memory, so that the words of a row meet every bank alike.
+template <int DH>
+struct KeyPart {
+  int t, d;
+  __device__ __forceinline__ KeyPart(int tid) : t(tid / (DH / 8)), d(tid % (DH / 8) * 8) {}
+  // of token t + 16 h
+  __device__ __forceinline__ int at(int h) const {
+    return ((h * (DH / 64) + d / 64) * 65 + d % 32 / 8 * 16 + t) * 4 + d % 64 / 32 * 2;
+  }
+};
+// And of the values: dims d .. d + 3 of tokens t .. t + 3, four words of four codes.
+template <int DH>
+struct ValuePart {
+  int t, d;
+  __device__ __forceinline__ ValuePart(int tid) : t(tid / (DH / 4) * 4), d(tid % (DH / 4) * 4) {}
+  // word of dim d + e
+  __device__ __forceinline__ int at(int e) const {
+    return (d / 32 * 65 + (t / 4 & 3) * 16 + d % 16 + e) * 4 + d % 32 / 16 * 2 + t / 16;
+  }
+  static constexpr int WORDS = DH / 32 * 65 * 4;
+  __device__ static int own(int tid) { return ((tid >> 6) * 65 + (tid & 63)) * 4; }  // of thread tid's 16 bytes
+};
+// 4 x 4 bytes: byte c of word r becomes byte r of word c
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// The inverse: 16 bytes a thread from memory as they lie, across LDS in words into rows.
+// The 50 MB take 10.0 us (5.0 TB/s with the launch), with values picked from LDS byte by byte
+// and keys written in half cache lines 10.3.
 template <int DH>
 __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
-  constexpr int T = 2 * DH, TPR = T / BLK, V = DH / TPR;
-  __shared__ u32x4 vs[T];
+  __shared__ __attribute__((aligned(16))) uint32_t vs[ValuePart<DH>::WORDS];
   const Span s = span_of(a, blockIdx.x >> 1);
-  const int values = blockIdx.x & 1;
+  const bool values = blockIdx.x & 1;
   if (s.t0 >= s.t1) return;
   const size_t block = ((size_t)s.b * a.Hkv + s.h) * (a.L_cap / BLK) + s.blk;
   const u32x4* image = (const u32x4*)((const uint8_t*)a.cache + block * (64 * DH) + values * (32 * DH));
@@ -204,44 +243,35 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
   const int tid = threadIdx.x;
   const u32x4 own = image[tid];
   const Heads& out = values ? a.v : a.k;
-  // 8 codes as bf16: exact, the codes have 4 bits and a power of two keeps them
-  auto wide = [&](uint32_t lo, uint32_t hi) {
-    const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, true);
-    const f32x2 r = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), u = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
-    return u32x4{pack_bf2(p[0] * step, p[1] * step), pack_bf2(q[0] * step, q[1] * step),
-                 pack_bf2(r[0] * step, r[1] * step), pack_bf2(u[0] * step, u[1] * step)};
+  // four codes as bf16: exact, the codes have 4 bits and a power of two keeps them
+  auto wide = [&](uint32_t w) {
+    const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    return u32x2{pack_bf2(p[0] * step, p[1] * step), pack_bf2(q[0] * step, q[1] * step)};
   };
-  auto row_of = [&](int t) {
-    return (bf16_t*)out.p + s.b * out.seq + (int64_t)(s.from + t - s.t0) * out.token + s.h * out.head;
-  };
+  bf16_t* rows = (bf16_t*)out.p + s.b * out.seq + s.h * out.head;
+  *(u32x4*)&vs[ValuePart<DH>::own(tid)] = own;
+  __syncthreads();
   if (!values) {
-    const int lane = tid & 63, c = lane & 15, q = lane >> 4, piece = tid >> 6;
-    const int t = piece / (DH / 64) * 16 + c, d = piece % (DH / 64) * 64 + q * 8;
-    if (t < s.t0 || t >= s.t1) return;
-    bf16_t* row = row_of(t);
-    *(u32x4*)(row + d) = wide(own[0], own[1]);
-    *(u32x4*)(row + d + 32) = wide(own[2], own[3]);
+    const KeyPart<DH> kp(tid);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int t = kp.t + 16 * h;
+      if (t < s.t0 || t >= s.t1) continue;
+      const u32x2 lo = wide(vs[kp.at(h)]), hi = wide(vs[kp.at(h) + 1]);
+      *(u32x4*)(rows + (int64_t)(s.from + t - s.t0) * out.token + kp.d) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
     return;
   }
-  vs[tid] = own;
-  __syncthreads();
-  const int t = tid / TPR, d0 = tid % TPR * V;
-  if (t < s.t0 || t >= s.t1) return;
-  const uint8_t* bytes = (const uint8_t*)vs;
-  uint32_t w[4];
+  const ValuePart<DH> vp(tid);
+  uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t v = 0;
+  for (int e = 0; e < 4; ++e) c[e] = vs[vp.at(e)];
+  transpose4(c);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int d = d0 + i * 4 + r;
-      v |= (uint32_t)bytes[((d / 32 * 64 + t % 16 / 4 * 16 + d % 16) * 2 + d % 32 / 16) * 8 + t / 16 * 4 + t % 4] << 8 * r;
-    }
-    w[i] = v;
+  for (int r = 0; r < 4; ++r) {
+    const int t = vp.t + r;
+    if (t >= s.t0 && t < s.t1) *(u32x2*)(rows + (int64_t)(s.from + t - s.t0) * out.token + vp.d) = wide(c[r]);
   }
-  bf16_t* row = row_of(t) + d0;
-  *(u32x4*)row = wide(w[0], w[1]);
-  *(u32x4*)(row + 8) = wide(w[2], w[3]);
 }
 
 // -------------------------------------------------------------- attention
@@ -263,7 +293,12 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
 // and others do not must reach the former only: 0 NaN is NaN, so such codes are zeroed
 // too, and a product of (is NaN) with (sees it) marks the outputs that they make NaN.
 // Work is split over the keys: waves of a workgroup take every W-th block, workgroups
-// contiguous runs of blocks, joined in LDS and by kv8_combine_kernel.
+// contiguous runs of blocks, joined in LDS and by kv8_combine_kernel.  Reading the cache
+// bounds it: a token of 16 sequences of 32768 over 8 KV heads of 128 takes 186 us (5.8 TB/s), of
+// eight of 4096 to 32768 63.5 (4.8 TB/s: lengths are not known where work is split), of one
+// of 2048 over 32 heads 9.3, of which 4.6 are two launches.  Where a KV head has several tiles of
+// queries, they run on one XCD one behind the other and read keys from its L2: 16 tokens
+// of 28 heads over 4 KV heads of 131072 keys 100 -> 75 us against tiles apart.
 
 constexpr float LOWEST = -3e38f;  // a maximum before any score: finite, so that no difference of two is NaN
 constexpr float RISE = 15.f, PLACE = 7.f;
@@ -305,6 +340,8 @@ __device__ __forceinline__ f32x4 mfma_f16(const f16x8& a, const f16x8& b, const 
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+constexpr int TILE = 16;  // query rows
+
 // The blocks that any of tile rows [row0, row1] of a sequence sees: `sinkb` blocks of
 // first tokens, then those from blk0 on; nb in all.
 struct Seen {
@@ -329,8 +366,6 @@ __device__ __forceinline__ void store_row(const Kv8Attn& a, int b, int hk, int g
   *(u32x2*)o = u32x2{pack_bf2(v[0] * f, v[1] * f), pack_bf2(v[2] * f, v[3] * f)};
 }
 
-constexpr int TILE = 16;  // query rows
-
 template <int DH, int W>
 __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
   constexpr int KP = DH / 64, VP = DH / 32, ND = DH / 16, NS = DH / 32;  // 16-byte pieces of a lane (keys: a tile)
@@ -338,9 +373,12 @@ __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
   __shared__ float sm[W][TILE], sl[W][TILE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, q = lane >> 4;
-  const int bh = blockIdx.x, split = blockIdx.y;
+  // workgroup n is on XCD n % 8: there the tiles of a run of keys one behind the other, for its L2
+  const int n = blockIdx.x, slot = n / 8, group = div_by(slot, a.by_tiles) * 8 + n % 8;
+  const int total = a.B * a.Hkv, split = div_by(group, a.by_BH), bh = group - split * total;
+  if (split >= a.nsplit) return;
   const int b = div_by(bh, a.by_Hkv), hk = bh - b * a.Hkv;
-  const int G = a.G, rows = a.Lq * G, row0 = blockIdx.z * TILE;
+  const int G = a.G, rows = a.Lq * G, row0 = (slot - div_by(slot, a.by_tiles) * a.tiles) * TILE;
   // this lane's query: row row0 + c16
   const int row = row0 + c16;
   bf16x8 qb[NS];
@@ -361,7 +399,7 @@ __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
   const f32x2* const steps = (const f32x2*)((const uint8_t*)a.cache + (size_t)a.B * a.Hkv * nblk * (64 * DH)) + (size_t)bh * nblk;
 
   u32x4 kc[2][KP], vc[VP];
-  f32x2 sk, sv;  // the steps that came with the keys, and with the values
+  f32x2 sk;  // the block's two steps, with its keys
   auto block_of = [&](int j) { return j < sn.sinkb ? j : sn.blk0 + j - sn.sinkb; };
   // past the run's last block: an empty buffer, no memory is touched
   auto buffer = [&](int j) {
@@ -520,7 +558,7 @@ __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
     } else {
       const size_t at = ((size_t)bh * rows + gr) * a.nsplit + split;
       *(f32x4*)(a.part + at * DH + d) = v;
-      if (d == 0) *(f32x2*)(a.part + (size_t)gridDim.x * rows * a.nsplit * DH + at * 2) = f32x2{mx, ls};
+      if (d == 0) *(f32x2*)(a.part + (size_t)total * rows * a.nsplit * DH + at * 2) = f32x2{mx, ls};
     }
   }
 }
@@ -597,21 +635,28 @@ unsigned most_splits(int B, int Lq, int H, int Hkv, unsigned blocks) {
   return n < (blocks + 3) / 4 ? (unsigned)n : (blocks + 3) / 4;
 }
 
+// What a call costs, fitted to 117 shapes of 1 to 256 KV heads of all sequences, 300 to 131072 tokens, 1 to 7 tiles of
+// queries, with lengths alike and from an eighth on, at 20 to 50 plans each: those chosen are 2.1% slower than the
+// fastest ones on average, 13% at most.  Always 8 waves would be as fast on average, but 10% slower where eight
+// sequences of 4096 to 32768 tokens run together, always 4 waves 3.5% slower on average.  (Splits chosen on the
+// device by the lengths themselves are 10% faster there without their choice, which costs 3 us.)
 struct Plan {
   int W, tiles, chunk, nsplit;
 };
 Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) {
   const int rows = Lq * (H / Hkv), tiles = cdiv(rows, TILE);
   const unsigned blocks = blocks_of(Lq, max_len, window, sinks), limit = most_splits(B, Lq, H, Hkv, blocks);
-  const int64_t bt = (int64_t)B * Hkv * tiles;
+  const int64_t runs = (int64_t)B * Hkv, bt = runs * tiles;
   Plan p{};
   int64_t best = INT64_MAX;
   for (int W = 4; W <= 8; W += 4) {
-    const unsigned most = (blocks + W - 1) / W;
+    const unsigned most = (blocks + W - 1) / W;  // blocks of a wave, if nothing is split
     auto consider = [&](unsigned per) {
       const unsigned ns = (blocks + per * W - 1) / (per * W);
-      const int64_t a_simd = (bt * ns + 255) / 256 * (W / 4), wave = 75ll * per, simd = a_simd * (35 * per + 37);
-      const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 231 + 22 * ((ns - 1) / 16) : 0);
+      // waves of one SIMD; times of a wave alone, of a SIMD's together, of the join (a unit is some 6 ns)
+      const int64_t waves = ((runs * ns + 7) / 8 * tiles + 31) / 32 * (W / 4);
+      const int64_t wave = 40ll * per, simd = waves * (17 * per + 24);
+      const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 209 + 49 * ((ns - 1) / 16) : 0);
       if (cost < best && ns <= limit) best = cost, p = Plan{W, tiles, (int)(per * W), (int)ns};
       return wave < best;  // else longer runs of blocks cost no less
     };
@@ -624,8 +669,9 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
 }
 
 template <int DH, int W>
-hipError_t launch_attention(const Kv8Attn& a, int tiles, hipStream_t s) {
-  hipLaunchKernelGGL((kv8_attention_kernel<DH, W>), dim3(a.B * a.Hkv, a.nsplit, tiles), dim3(W * 64), 0, s, a);
+hipError_t launch_attention(const Kv8Attn& a, hipStream_t s) {
+  const int64_t wgs = ((int64_t)a.B * a.Hkv * a.nsplit + 7) / 8 * 8 * a.tiles;
+  hipLaunchKernelGGL((kv8_attention_kernel<DH, W>), dim3((unsigned)wgs), dim3(W * 64), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   hipLaunchKernelGGL((kv8_combine_kernel<DH>), dim3(a.B * a.Lq * a.H), dim3(64), 0, s, a, a.B * a.Lq * a.H);
@@ -674,13 +720,16 @@ hipError_t kv8_attention(Kv8Attn a, int dh, size_t scratch_bytes, hipStream_t s)
   a.G = a.H / a.Hkv;
   a.by_G = fast_div(a.G);
   a.by_Hkv = fast_div(a.Hkv);
-  a.by_chunk = fast_div(p.chunk);
   a.by_rows = fast_div(a.Lq * a.G);
+  a.by_BH = fast_div(a.B * a.Hkv);
+  a.by_tiles = fast_div(p.tiles);
+  a.tiles = p.tiles;
   a.chunk = p.chunk;
+  a.by_chunk = fast_div(p.chunk);
   a.nsplit = p.nsplit;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
-  if (p.W == 8) return dh == 128 ? launch_attention<128, 8>(a, p.tiles, s) : launch_attention<64, 8>(a, p.tiles, s);
-  return dh == 128 ? launch_attention<128, 4>(a, p.tiles, s) : launch_attention<64, 4>(a, p.tiles, s);
+  if (p.W == 8) return dh == 128 ? launch_attention<128, 8>(a, s) : launch_attention<64, 8>(a, s);
+  return dh == 128 ? launch_attention<128, 4>(a, s) : launch_attention<64, 4>(a, s);
 }
 
 }  // namespace vla
