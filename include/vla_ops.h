@@ -264,6 +264,8 @@ vla_status vla_op_attention_packed(const vla_heads *q, const vla_heads *k, const
  * finite is held as NaN and does not move e.
  * load takes rows out into k, v, 2^e c rounded to bf16 (exact).  Positions outside [0, L_cap) are
  * left out; other blocks of the cache (store) and rows of k, v (load) stay as they were.
+ * Prompts packed behind one another are stored in one call as sequences that share
+ * all rows: seq 0, start[b] = -offsets[b], count[b] = offsets[b + 1].
  * A call may touch one sequence's slot once; calls on one cache must be ordered
  * (one stream).  L_cap % 32 == 0, L_cap <= 2^24, dh in {64, 128}.
  * vla_op_kv8_bytes is 0 for sizes that are refused. */
