@@ -105,6 +105,29 @@ def test_norm_i8_rows_that_are_not_finite_or_zero():
             assert np.array_equal(c[5:], code) and np.all(np.abs(s[5:] - scale) <= 64 * U32 * scale)
 
 
+@pytest.mark.parametrize("d", [64, 1000, 4096, 11008, 32768])
+@pytest.mark.parametrize("add", ["", "f32", "bf16", "into x", "into add"])
+def test_norm_i8_rows_whose_squares_leave_fp32(d, add):
+    rng = _rng(6, d)
+    size = np.array([1e25, 1.0, 1e-25, 1e19, 3e-21, 1e37], np.float32)[:, None]
+    x = rng.standard_normal((6, d)).astype(np.float32) * size / 8
+    g = rng.uniform(0.5, 1.5, d).astype(np.float32)
+    y = None if not add else (rng.standard_normal((6, d)).astype(np.float32) * size / 8)
+    xd, yd = _cuda(x), None if y is None else _cuda(y)
+    if add == "bf16":
+        yd = yd.bfloat16()
+        y = yd.float().cpu().numpy()
+    total = {"into x": xd, "into add": yd}.get(add)
+    codes, scales = torch.empty((6, d), dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda")
+    for eps in (0.0, 1e-6):
+        if total is not None:
+            xd.copy_(_cuda(x)), yd.copy_(_cuda(y))
+        vb.vla_op_norm_i8(xd, yd, total, _cuda(g), eps, codes, scales)
+        _, code, scale = _ref_norm(x, y, g, eps)
+        assert np.array_equal(codes.cpu().numpy(), code)
+        assert np.all(np.abs(scales.cpu().numpy() - scale) <= 64 * U32 * scale)
+
+
 def test_norm_i8_in_place():
     """The sum may go to x itself, or to add, and twice the same call gives the same bits."""
     rng = _rng(3)
