@@ -98,7 +98,8 @@ __device__ __forceinline__ void by_output(const GemmI8Args& a, F f) {
 // Up to 16 rows of x: the weights' bytes are the bound.  A workgroup takes NT tiles of
 // weight rows (SWIGLU: NT / 2 gate tiles and the up tiles of the same features); its W
 // waves take runs of U steps in turn and add up in LDS.  Weights and x go from memory
-// into registers, a run ahead.
+// into registers, a run ahead.  One row, 12288 x 4096: 9.6 us, 11.7 with the weights
+// from memory (5.4 TB/s behind the launch's 2.3 us).
 template <int NT, int W, int U, bool SWIGLU>
 __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
   __shared__ i32x4 part[W][NT][64];
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
 // What bounds it is how fast a CU is filled, 70 GB/s or 33 bytes a cycle in whole cache
 // lines: (BM + BN) 64 bytes a step against BM BN / 64 cycles of MFMAs (8192 operations a
 // cycle and CU).  With 64 bytes of a row of x a load, in place of the 128 of a cache line,
-// x counted twice (333 x 4096, K = 11008 38 us, now 29).
+// x counted twice (333 x 4096, K = 11008 38 us, now 27).
 template <int BM, int BN, int WGN, int KG, int NX, int D, int LA, bool SWIGLU>
 __global__ __launch_bounds__(64 * WGN * KG) void w8_tile_kernel(GemmI8Args a) {
   constexpr int NW = WGN * KG, TM = BM / 16, TN = BN / WGN / 16, SP = 2 / KG;  // own steps a slab
