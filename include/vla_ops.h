@@ -227,8 +227,8 @@ vla_status vla_op_w8_pack(const void *codes, const float *scales, void *Wp, int 
  * swiglu: W holds N / 2 gate rows, then the N / 2 up rows, and out[M][N / 2] =
  * silu(x Wgate^T) * (x Wup^T) + residual; N % 64 == 0.
  * Row strides in elements, no less than a row's width where M > 1: ldx of x (a
- * multiple of 16; x 16-byte aligned), ldo of out and of residual, which may be the
- * same memory (fp32 out).  A scale of x that is not finite gives a row of out that is
+ * multiple of 16, up to 2^22; x 16-byte aligned), ldo of out and of residual (up to
+ * 2^20), which may be the same memory (fp32 out).  A scale of x that is not finite gives a row of out that is
  * not finite, and reaches no other row. */
 vla_status vla_op_gemm_i8(const void *x, int64_t ldx, const float *sx, const void *Wp, const float *residual, void *out,
                           int64_t ldo, vla_dtype out_dtype, int swiglu, int M, int N, int K, void *stream);

@@ -33,6 +33,9 @@ __device__ __forceinline__ i32x4 mfma_i8(const i32x4& a, const i32x4& b, const i
 }
 __device__ __forceinline__ float silu_of(float g) { return g / (1.f + __expf(-g)); }
 
+// (The range check of a buffer counts the scalar offset too, also where that alone lies past the end: such loads gave
+// zeros in every combination tried.)
+
 // Rows [m0, m0 + rows) of out and of the residual as buffers: a store past them, or one
 // to NOWHERE, is dropped, so the epilogue has no branches.  WIDE: four outputs side by
 // side exist together, and rows are aligned for them.

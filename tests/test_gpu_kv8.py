@@ -207,6 +207,22 @@ def test_attention(dh, H, Hkv, Lq):
         _check(_attend(q, cache, L_cap, Hkv, lens, max_len), q, held, lens)
 
 
+@pytest.mark.parametrize("dh,B,H,Hkv,Lq,lens,window,sinks", [
+    (64, 1, 21, 3, 16, [6001], 0, 0), (128, 3, 14, 1, 9, [4100, 9, 2500], 0, 0), (64, 2, 40, 1, 7, [3333, 0], 0, 0),
+    (128, 1, 5, 5, 40, [3000], 0, 0), (64, 1, 21, 3, 16, [6001], 1500, 40), (128, 9, 16, 1, 2, [700, 1, 2900, 33, 64, 1500, 2, 0, 2222], 0, 0)])
+def test_attention_tiles_and_splits(dh, B, H, Hkv, Lq, lens, window, sinks):
+    """Several tiles of queries over keys that several workgroups share, their numbers no multiples of eight."""
+    L = max(lens)
+    L_cap = (L + 31) // 32 * 32
+    k, v = _kv(("tiles", H, Lq, dh), B, L, Hkv, dh)
+    q = ref.normal(("tilesq", H, Lq, dh), (B, Lq, H, dh))
+    cache, held = _filled(k, v, L_cap, lens)
+    assert _vb().vla_op_attention_kv8_scratch(B, Lq, H, Hkv, dh, L, window, sinks) > 0
+    o = _attend(q, cache, L_cap, Hkv, lens, L, window, sinks)
+    _check(o, q, held, lens, window, sinks)
+    assert np.array_equal(o, _attend(q, cache, L_cap, Hkv, lens, L, window, sinks))
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (5, 0), (32, 4), (33, 40), (100, 1), (250, 16), (699, 3), (5000, 2)])
 def test_attention_window(window, sinks):
     lens = [3, 40, 333, 600]
