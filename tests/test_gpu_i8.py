@@ -128,6 +128,25 @@ def test_norm_i8_rows_whose_squares_leave_fp32(d, add):
         assert np.all(np.abs(scales.cpu().numpy() - scale) <= 64 * U32 * scale)
 
 
+@pytest.mark.parametrize("xt,at", [("bf16", "f32"), ("bf16", "bf16"), ("f32", None), ("bf16", None)])
+@pytest.mark.parametrize("norm", [True, False])
+def test_norm_i8_other_types(xt, at, norm):
+    """Gain with bf16 rows, and a sum that is asked for where nothing is added."""
+    rng = _rng(7, norm)
+    M, d = 37, 1032
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}
+    x = _cuda(rng.standard_normal((M, d)).astype(np.float32)).to(dt[xt])
+    add = _cuda(rng.standard_normal((M, d)).astype(np.float32)).to(dt[at]) if at else None
+    g = _cuda(rng.uniform(0.5, 1.5, d).astype(np.float32)) if norm else None
+    codes, scales = torch.empty((M, d), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    total = torch.empty((M, d), device="cuda")
+    vb.vla_op_norm_i8(x, add, total, g, 0.25, codes, scales)
+    t, code, scale = _ref_norm(x.float().cpu().numpy(), None if add is None else add.float().cpu().numpy(),
+                               None if g is None else g.cpu().numpy(), 0.25)
+    assert np.array_equal(codes.cpu().numpy(), code) and np.array_equal(total.cpu().numpy(), t)
+    assert np.all(np.abs(scales.cpu().numpy() - scale) <= 64 * U32 * scale)
+
+
 def test_norm_i8_in_place():
     """The sum may go to x itself, or to add, and twice the same call gives the same bits."""
     rng = _rng(3)
@@ -225,6 +244,45 @@ def test_gemm_i8_tiles(tile):
 def test_gemm_i8_large(M, N, K):
     _product(M, N, K, "bf16")
     _product(M, N, K, "add", seed=1, wide=4)
+
+
+@pytest.mark.parametrize("M", [1, 16, 17, 100, 700])
+@pytest.mark.parametrize("swiglu", [False, True])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_gemm_i8_residuals(M, swiglu, dt):
+    """A residual behind the gate, and one of its own memory for either output."""
+    rng = _rng(8, M)
+    N, K = 320, 528
+    cols = N // 2 if swiglu else N
+    x, w = rng.integers(-128, 128, (M, K), dtype=np.int8), rng.integers(-128, 128, (N, K), dtype=np.int8)
+    sx, sw = rng.uniform(0.5, 2, M).astype(np.float32), (rng.uniform(0.5, 2, N) / (5000 * np.sqrt(K))).astype(np.float32)
+    for wide in (0, 3):
+        r, _ = _strided((M, cols), torch.float32, wide, 1.0)
+        r.copy_(_cuda(rng.standard_normal((M, cols)).astype(np.float32)))
+        o, whole = _strided((M, cols), dt, wide, 3.0)
+        vb.vla_op_gemm_i8(_cuda(x), _cuda(sx), _pack(w, sw), r, o, N, swiglu)
+        y, res = _ref_gemm(x, sx, w, sw, swiglu), r.cpu().numpy().astype(np.float64)
+        own = np.abs(y) * (2.0 ** -17 if swiglu else 4 * U32) + 1e-37
+        tol = own + np.abs(y + res) * (U32 if dt == torch.float32 else UB + U32)
+        assert np.all(np.abs(o.double().cpu().numpy() - (y + res)) <= tol * (1 + 2.0 ** -8))
+        assert bool((whole[:, cols:] == 3.0).all())
+
+
+def test_nothing_to_do():
+    """Tensors without rows, tokens or sequences."""
+    e = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+    Wp = torch.zeros(vb.vla_op_w8_packed_bytes(64, 64), dtype=torch.uint8, device="cuda")
+    vb.vla_op_norm_i8(e(0, 64), None, None, None, 0.0, e(0, 64, dtype=torch.int8), e(0, dtype=torch.float32))
+    vb.vla_op_gemm_i8(e(0, 64, dtype=torch.int8), e(0, dtype=torch.float32), Wp, None, e(0, 64), 64)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    vb.vla_op_attention_packed(e(0, 4, 64), e(0, 2, 64), e(0, 2, 64), i32(0, 0), e(0, 4, 64))
+    o = torch.full((5, 4, 64), 2.0, dtype=torch.bfloat16, device="cuda")
+    vb.vla_op_attention_packed(o, o[:, :2], o[:, 2:], i32(0), o.clone())
+    cache = torch.zeros(vb.vla_op_kv8_bytes(2, 2, 32, 64), dtype=torch.uint8, device="cuda")
+    vb.vla_op_kv8_store(e(2, 0, 2, 64), e(2, 0, 2, 64), i32(0, 0), None, cache, 32)
+    vb.vla_op_kv8_load(cache, 32, i32(0, 0), None, e(2, 0, 2, 64), e(2, 0, 2, 64))
+    vb.vla_op_attention_kv8(e(2, 0, 4, 64), cache, 32, 2, i32(1, 1), e(2, 0, 4, 64), 32)
+    assert not bool(cache.any())
 
 
 def test_gemm_i8_extremes():
