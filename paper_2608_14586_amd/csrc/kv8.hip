@@ -639,7 +639,8 @@ unsigned most_splits(int B, int Lq, int H, int Hkv, unsigned blocks) {
 // queries, with lengths alike and from an eighth on, at 20 to 50 plans each: those chosen are 2.1% slower than the
 // fastest ones on average, 13% at most.  Always 8 waves would be as fast on average, but 10% slower where eight
 // sequences of 4096 to 32768 tokens run together, always 4 waves 3.5% slower on average.  (Splits chosen on the
-// device by the lengths themselves are 10% faster there without their choice, which costs 3 us.)
+// device by the lengths themselves, from one sum over the sequences, are 4% faster to 30% slower there: workgroups
+// whose sequence ends before them make room for the others as it is.)
 struct Plan {
   int W, tiles, chunk, nsplit;
 };
@@ -653,7 +654,7 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
     const unsigned most = (blocks + W - 1) / W;  // blocks of a wave, if nothing is split
     auto consider = [&](unsigned per) {
       const unsigned ns = (blocks + per * W - 1) / (per * W);
-      // waves of one SIMD; times of a wave alone, of a SIMD's together, of the join (a unit is some 6 ns)
+      // waves of one SIMD; times of a wave alone, of a SIMD's together, of the join (a unit is some 20 ns)
       const int64_t waves = ((runs * ns + 7) / 8 * tiles + 31) / 32 * (W / 4);
       const int64_t wave = 40ll * per, simd = waves * (17 * per + 24);
       const int64_t cost = (wave > simd ? wave : simd) + (ns > 1 ? 209 + 49 * ((ns - 1) / 16) : 0);
