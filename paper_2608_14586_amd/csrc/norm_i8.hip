@@ -14,7 +14,7 @@
 // Bound by memory: the row stays in registers between its reductions and its
 // codes.  2048 rows of 4096, the fp32 residual with a bf16 addition, written back, 92 MB:
 // 19.8 us (4.7 TB/s, the launch's 2.3 us included), 23 with nothing in a cache; 1777 rows
-// 14.4 without the residual written back; 4 rows 2.9, which is the launch.
+// of 11008 in bf16 without a gain 14.0; 4 rows 2.9, which is the launch.
 //
 // The sum of squares is fp32.  Where it leaves what fp32 holds well (rows near 2^64 and
 // above, or 2^-40 and below) it is taken again in 64 bits.
@@ -52,8 +52,8 @@ __device__ __forceinline__ double wave_sum(double x) {
   return x;
 }
 
-// One row per workgroup of T threads, NV pieces of 8 values a thread.
-template <int T, int NV>
+// One row per workgroup of T threads, NV pieces of 8 values a thread; NORM: with a gain.
+template <int T, int NV, bool NORM>
 __global__ __launch_bounds__(T) void norm_i8_kernel(NormI8Args p) {
   constexpr int W = T / 64;
   __shared__ uint32_t tops[W];
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(T) void norm_i8_kernel(NormI8Args p) {
         *(f32x4*)s = f32x4{u[v][0], u[v][1], u[v][2], u[v][3]};
         *(f32x4*)(s + 4) = f32x4{u[v][4], u[v][5], u[v][6], u[v][7]};
       }
-      if (p.g) {
+      if constexpr (NORM) {
         float g[8];
         load8(p.g, i * 8, true, g);
 #pragma unroll
@@ -101,56 +101,53 @@ __global__ __launch_bounds__(T) void norm_i8_kernel(NormI8Args p) {
     }
   }
   top = wave_max_u(top);
-  ss = warp_sum(ss);
+  if constexpr (NORM) ss = warp_sum(ss);
   if constexpr (W > 1) {
     if (lane == 0) {
       tops[wave] = top;
-      sums[wave] = ss;
+      if constexpr (NORM) sums[wave] = ss;
     }
     __syncthreads();
     top = tops[0];
-    ss = sums[0];
+    if constexpr (NORM) ss = sums[0];
 #pragma unroll
     for (int w = 1; w < W; ++w) {
       top = max(top, tops[w]);
-      ss += sums[w];
+      if constexpr (NORM) ss += sums[w];
     }
   }
   const bool finite = top < 0x7f800000u;
   float a = __uint_as_float(top);
   if (!finite || a < 0x1p-100f) a = 0.f;  // codes of zero, the scale NaN or zero
   const float inv = a > 0.f ? 127.f / a : 0.f;
-  float factor = 1.f;
-  if (p.g && a > 0.f) {
-    factor = 1.f / sqrtf(ss / (float)p.d + p.eps);
-    if (!(ss >= 0x1p-80f && ss < INFINITY)) {  // the whole workgroup
-      __shared__ double wide[W];
-      double sq = 0.0;
+  const bool again = NORM && a > 0.f && !(ss >= 0x1p-80f && ss < INFINITY);
+  double sq = 0.0;
+  if (again) {  // the whole workgroup
+    __shared__ double wide[W];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int i = tid + v * T;
-        if (i >= nv) continue;
-        float t[8], y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (p.sum) {  // what this thread wrote; x or add may be the same memory
-          load8(p.sum, row * p.ldsum + i * 8, true, t);
-        } else {
-          load8(p.x, row * p.ldx + i * 8, p.x_f32, t);
-          if (p.add) load8(p.add, row * p.ldadd + i * 8, p.add_f32, y);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq += (double)(t[e] + y[e]) * (double)(t[e] + y[e]);
+    for (int v = 0; v < NV; ++v) {
+      const int i = tid + v * T;
+      if (i >= nv) continue;
+      float t[8], y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (p.sum) {  // what this thread wrote; x or add may be the same memory
+        load8(p.sum, row * p.ldsum + i * 8, true, t);
+      } else {
+        load8(p.x, row * p.ldx + i * 8, p.x_f32, t);
+        if (p.add) load8(p.add, row * p.ldadd + i * 8, p.add_f32, y);
       }
-      sq = wave_sum(sq);
-      if (lane == 0) wide[wave] = sq;
-      __syncthreads();
-      sq = 0.0;
 #pragma unroll
-      for (int w = 0; w < W; ++w) sq += wide[w];
-      factor = (float)(1.0 / sqrt(sq / p.d + (double)p.eps));
+      for (int e = 0; e < 8; ++e) sq += (double)(t[e] + y[e]) * (double)(t[e] + y[e]);
     }
+    sq = wave_sum(sq);
+    if (lane == 0) wide[wave] = sq;
+    __syncthreads();
+    sq = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) sq += wide[w];
   }
   if (tid == 0) {
-    const float s = a * (1.f / 127.f) * factor;
+    float s = a * (1.f / 127.f);
+    if (NORM && a > 0.f) s *= again ? (float)(1.0 / sqrt(sq / p.d + (double)p.eps)) : 1.f / sqrtf(ss / (float)p.d + p.eps);
     p.scales[row] = finite ? s : __uint_as_float(0x7fc00000u);
   }
 #pragma unroll
@@ -185,7 +182,10 @@ __global__ __launch_bounds__(T) void norm_i8_kernel(NormI8Args p) {
 
 template <int T, int NV>
 hipError_t launch(const NormI8Args& a, int M, hipStream_t s) {
-  hipLaunchKernelGGL((norm_i8_kernel<T, NV>), dim3(M), dim3(T), 0, s, a);
+  if (a.g)
+    hipLaunchKernelGGL((norm_i8_kernel<T, NV, true>), dim3(M), dim3(T), 0, s, a);
+  else
+    hipLaunchKernelGGL((norm_i8_kernel<T, NV, false>), dim3(M), dim3(T), 0, s, a);
   return hipGetLastError();
 }
 
