@@ -27,7 +27,9 @@
 // half of its weights between the PV products (16384 tokens 4% faster, prompts of 2048 4%
 // slower), a third stage of values (0 to 10% slower), and key tiles dealt out to two groups of four
 // waves (10 to 18% faster where fewer than 256 workgroups have 15 tiles and more, else slower;
-// and a prompt's bits would depend on the others of the call).
+// and a prompt's bits would depend on the others of the call), nor 64 queries a workgroup with two waves
+// on the halves of each key tile, for prompts of up to 1024 (14 heads of 64: one of 1024 16.5 -> 12.8 us,
+// nine of 1 to 701 12.9 -> 12.2, but 64 of 512 77 -> 102).
 //
 // Only a wave's last tile has masked keys, in one half of its 64 (the other is seen by all of
 // the wave's queries, or by none).  A value there that is not finite must not reach the
