@@ -373,12 +373,17 @@ __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
   __shared__ float sm[W][TILE], sl[W][TILE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, q = lane >> 4;
-  // workgroup n is on XCD n % 8: there the tiles of a run of keys one behind the other, for its L2
-  const int n = blockIdx.x, slot = n / 8, group = div_by(slot, a.by_tiles) * 8 + n % 8;
-  const int total = a.B * a.Hkv, split = div_by(group, a.by_BH), bh = group - split * total;
-  if (split >= a.nsplit) return;
+  const int total = a.B * a.Hkv;
+  int bh = blockIdx.x, split = blockIdx.y, row0 = 0;
+  if (a.tiles > 1) {  // workgroup n is on XCD n % 8: there the tiles of a run of keys one behind the other, for its L2
+    const int slot = bh / 8, at = div_by(slot, a.by_tiles), group = at * 8 + bh % 8;
+    split = div_by(group, a.by_BH);
+    if (split >= a.nsplit) return;
+    bh = group - split * total;
+    row0 = (slot - at * a.tiles) * TILE;
+  }
   const int b = div_by(bh, a.by_Hkv), hk = bh - b * a.Hkv;
-  const int G = a.G, rows = a.Lq * G, row0 = (slot - div_by(slot, a.by_tiles) * a.tiles) * TILE;
+  const int G = a.G, rows = a.Lq * G;
   // this lane's query: row row0 + c16
   const int row = row0 + c16;
   bf16x8 qb[NS];
@@ -671,8 +676,9 @@ Plan plan_of(int B, int Lq, int H, int Hkv, int max_len, int window, int sinks) 
 
 template <int DH, int W>
 hipError_t launch_attention(const Kv8Attn& a, hipStream_t s) {
-  const int64_t wgs = ((int64_t)a.B * a.Hkv * a.nsplit + 7) / 8 * 8 * a.tiles;
-  hipLaunchKernelGGL((kv8_attention_kernel<DH, W>), dim3((unsigned)wgs), dim3(W * 64), 0, s, a);
+  const int64_t runs = (int64_t)a.B * a.Hkv;
+  const dim3 grid = a.tiles > 1 ? dim3((unsigned)((runs * a.nsplit + 7) / 8 * 8 * a.tiles)) : dim3((unsigned)runs, a.nsplit);
+  hipLaunchKernelGGL((kv8_attention_kernel<DH, W>), grid, dim3(W * 64), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   hipLaunchKernelGGL((kv8_combine_kernel<DH>), dim3(a.B * a.Lq * a.H), dim3(64), 0, s, a, a.B * a.Lq * a.H);
