@@ -295,8 +295,8 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
 // Work is split over the keys: waves of a workgroup take every W-th block, workgroups
 // contiguous runs of blocks, joined in LDS and by kv8_combine_kernel.  Reading the cache
 // bounds it: a token of 16 sequences of 32768 over 8 KV heads of 128 takes 186 us (5.8 TB/s), of
-// eight of 4096 to 32768 63.5 (4.8 TB/s: lengths are not known where work is split), of one
-// of 2048 over 32 heads 9.3, of which 4.6 are two launches.  Where a KV head has several tiles of
+// eight of 4096 to 32768 63 (4.8 TB/s: lengths are not known where work is split), of one
+// of 2048 over 32 heads 9.0, of which 4.6 are two launches.  Where a KV head has several tiles of
 // queries, they run on one XCD one behind the other and read keys from its L2: 16 tokens
 // of 28 heads over 4 KV heads of 131072 keys 100 -> 75 us against tiles apart.
 
