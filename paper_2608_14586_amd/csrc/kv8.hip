@@ -296,7 +296,7 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
 // contiguous runs of blocks, joined in LDS and by kv8_combine_kernel.  Reading the cache
 // bounds it: a token of 16 sequences of 32768 over 8 KV heads of 128 takes 186 us (5.8 TB/s), of
 // eight of 4096 to 32768 63 (4.8 TB/s: lengths are not known where work is split), of one
-// of 2048 over 32 heads 9.0, of which 4.6 are two launches.  Where a KV head has several tiles of
+// of 2048 over 32 heads 9.1, of which 4.6 are two launches.  Where a KV head has several tiles of
 // queries, they run on one XCD one behind the other and read keys from its L2: 16 tokens
 // of 28 heads over 4 KV heads of 131072 keys 100 -> 75 us against tiles apart.
 
@@ -562,8 +562,18 @@ __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
       store_row(a, b, hk, gr, d, v, ls);
     } else {
       const size_t at = ((size_t)bh * rows + gr) * a.nsplit + split;
-      *(f32x4*)(a.part + at * DH + d) = v;
-      if (d == 0) *(f32x2*)(a.part + (size_t)total * rows * a.nsplit * DH + at * 2) = f32x2{mx, ls};
+      const size_t ml = (size_t)total * rows * a.nsplit * DH + at * 2;
+      if (a.tiles > 1) {
+        // Past the caches (sc0, sc1), below 2^27 bytes in all: what L2 holds at the kernel's end must still be written
+        // back.  9 tokens of four sequences of 4096, 7 heads a KV head: 11.6 -> 10.2 us, such calls 2.3% on average;
+        // calls of one tile lose 0.5%.
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)a.part, (short)0, 0x7fffffff, 0x00020000);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, (uint32_t)((at * DH + d) * 4), 0, 17);
+        if (d == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{mx, ls}), r, (uint32_t)(ml * 4), 0, 17);
+      } else {
+        *(f32x4*)(a.part + at * DH + d) = v;
+        if (d == 0) *(f32x2*)(a.part + ml) = f32x2{mx, ls};
+      }
     }
   }
 }
