@@ -330,7 +330,7 @@ def test_large_scores_one_key_each():
     _check(_attend(q, cache, L_cap, Hkv, [L], L), q, held, [L])
 
 
-def test_row_bits_do_not_depend_on_the_batch_and_repeat():
+def test_calls_repeat_their_bits():
     lens = [100, 700, 350]
     k, v = _kv(("bits",), 3, 700, 2, 128)
     q = ref.normal(("bitsq",), (3, 1, 8, 128))
