@@ -44,6 +44,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "packed_order.h"
 
 namespace vla {
 namespace {
@@ -79,11 +80,9 @@ __device__ __forceinline__ int wave_sum_i(int v) {
 
 // The tile of BQ queries and the head (of H, some order) of workgroup `wg`: prompt rows
 // [start, start + len), queries from q0 on; len = 0 where there is no such tile.  Up to 64
-// prompts, tiles come longest first, all heads of one side by side: tile number n of a
-// prompt has n + 1 tiles' work, and F(n) = sum over prompts of max(tiles - n, 0) tiles have
-// number n or more.  Where all workgroups run at once, workgroup i and i + 256 on one CU, a
-// CU's two are a long and a short one, and the longest have a CU alone (32 heads of 128, one
-// prompt of 2048: 47 us, in plain order 49).  More prompts: one behind the other.
+// prompts, tiles come longest first, all heads of one side by side, in the order of packed_rank: tile
+// number n of a prompt has n + 1 tiles' work, and F(n) = sum over prompts of max(tiles - n, 0) tiles have
+// number n or more.  More prompts: one behind the other.
 struct Work {
   int start, len, q0, head;
 };
@@ -102,20 +101,11 @@ __device__ __forceinline__ Work work_of(const PackedAttn& p, int wg, int BQ) {
   int start, len, nt, pick = -1, tile = 0, id;
   if (n_seq <= 64) {
     nt = lane_seq(0, start, len);
-    const int total = wave_sum_i(nt), all = total * H;  // the launch has at least as many, below 2^24
-    int rank = wg;
-    if (all > 256 && all <= 512) {
-      const int twice = all - 256;  // CUs with two
-      if (wg < 256) {
-        rank = wg < twice ? 256 - twice + wg : wg - twice;
-      } else {  // whole tiles from the shortest on, then what the first 256 left of theirs
-        const int e = wg - 256, whole = (total - 1 - div_by(256, p.by_H)) * H, t = div_by(e, p.by_H);
-        rank = e < whole ? (total - 1 - t) * H + e - t * H : 256 + e - whole;
-      }
-    }
+    // total * H: the launch has at least as many workgroups, below 2^24
+    const int rank = packed_rank(wg, wave_sum_i(nt), H, [&](int n) { return div_by(n, p.by_H); });
+    if (rank < 0) return w;
     id = div_by(rank, p.by_H);
     w.head = rank - id * H;
-    if (total <= id) return w;
     int lo = 0, hi = (T + BQ - 1) / BQ, more = 0;  // F(lo) > id >= F(hi) = more
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2, f = wave_sum_i(max(nt - mid, 0));
