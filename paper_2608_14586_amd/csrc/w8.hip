@@ -33,8 +33,8 @@ __device__ __forceinline__ i32x4 mfma_i8(const i32x4& a, const i32x4& b, const i
 }
 __device__ __forceinline__ float silu_of(float g) { return g / (1.f + __expf(-g)); }
 
-// (The range check of a buffer counts the scalar offset too, also where that alone lies past the end: such loads gave
-// zeros in every combination tried.)
+// What a buffer's range check must cut is in the vector offset or in the buffer's own start and size; scalar offsets are 0
+// throughout, since a check need not count them.
 
 // Rows [m0, m0 + rows) of out and of the residual as buffers: a store past them, or one
 // to NOWHERE, is dropped, so the epilogue has no branches.  WIDE: four outputs side by
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
     wt[i] = a.wp + (size_t)t * KS * 1024;
   }
   // past the row of x: its next one, or zeros past the last; the weights there are zero
-  const uint32_t xbytes = (uint32_t)((a.M - 1) * a.ldx + a.K);
+  const int xbytes = (int)((a.M - 1) * a.ldx + a.K);
   const uint32_t xat = c16 < a.M ? (uint32_t)(c16 * a.ldx) + q * 16 : NOWHERE;
   i32x4 wr[2][NT][U], xr[2][U];
   auto fetch = [&](int b, int s0) {
@@ -129,12 +129,13 @@ __global__ __launch_bounds__(W * 64) void w8_rows_kernel(GemmI8Args a) {
       for (int i = 0; i < NT; ++i)
         wr[b][i][u] = __builtin_bit_cast(
             i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                       __builtin_amdgcn_make_buffer_rsrc((void*)wt[i], (short)0, in ? KS * 1024 : 0, 0x00020000),
-                       lane * 16, in ? (s0 + u) * 1024 : 0, 0));
+                       __builtin_amdgcn_make_buffer_rsrc((void*)(wt[i] + (s0 + u) * 1024), (short)0, in ? 1024 : 0, 0x00020000),
+                       lane * 16, 0, 0));
+      const int k = (s0 + u) * 64;  // may lie past the row's end, where the weights' steps are padded
       xr[b][u] = __builtin_bit_cast(
           i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                     __builtin_amdgcn_make_buffer_rsrc((void*)a.x, (short)0, in ? (int)xbytes : 0, 0x00020000), xat,
-                     in ? (s0 + u) * 64 : 0, 0));
+                     __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + k), (short)0, in ? max(xbytes - k, 0) : 0, 0x00020000),
+                     xat, 0, 0));
     }
   };
   i32x4 acc[NT];
@@ -209,7 +210,7 @@ template <int BM, int BN, int WGN, int KG, int NX, int D, int LA, bool SWIGLU>
 __global__ __launch_bounds__(64 * WGN * KG) void w8_tile_kernel(GemmI8Args a) {
   constexpr int NW = WGN * KG, TM = BM / 16, TN = BN / WGN / 16, SP = 2 / KG;  // own steps a slab
   constexpr int XB = BM / 8, PX = (XB + NW - 1) / NW, XS = XB * 1024;            // 1 KB loads of a slab of x
-  static_assert(PX == 1 || (PX % 2 == 0 && PX * NW == XB), "a load's half of 16 rows is known");
+  static_assert(PX <= 2, "offsets of a slab's loads");
   static_assert(TM % LA == 0 && D % SP == 0 && (NX - 1) * PX + D * TN < 64, "unrolling, vmcnt range");
   static_assert(!SWIGLU || TN % 2 == 0, "a wave's tiles must be whole (gate, up) pairs");
   constexpr int RED = KG > 1 ? WGN * TM * TN * 1024 : 0;
@@ -237,18 +238,20 @@ __global__ __launch_bounds__(64 * WGN * KG) void w8_tile_kernel(GemmI8Args a) {
   const int xbytes = (int)((rows - 1) * a.ldx + a.K);
   uint32_t xvoff[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    xvoff[h] = (uint32_t)((lane >> 3) * a.ldx) + ((lane & 7) ^ (4 * (PX == 1 ? wave & 1 : h) + (lane >> 4))) * 16;
+  for (int j = 0; j < PX; ++j) {
+    const int blk = wave * PX + j;
+    xvoff[j] = (uint32_t)((blk * 8 + (lane >> 3)) * a.ldx) + ((lane & 7) ^ (4 * (blk & 1) + (lane >> 4))) * 16;
+  }
   auto issue_x = [&](int slab, char* st) {
     // past the last slab: an empty buffer, no memory is touched
-    const __amdgpu_buffer_rsrc_t rx =
-        __builtin_amdgcn_make_buffer_rsrc((void*)xp, (short)0, 2 * slab < KS ? xbytes : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(xp + slab * 128), (short)0, 2 * slab < KS ? max(xbytes - slab * 128, 0) : 0, 0x00020000);
 #pragma unroll
     for (int j = 0; j < PX; ++j) {
       const int blk = wave * PX + j;
       if (PX * NW == XB || blk < XB)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void*)(st + blk * 1024), 16,
-                                                 xvoff[j & 1], (int)(blk * 8 * a.ldx) + slab * 128, 0, 0);
+                                                 xvoff[j], 0, 0, 0);
     }
   };
   // W: SWIGLU takes gate and up tiles of the same features in turn
@@ -265,7 +268,7 @@ __global__ __launch_bounds__(64 * WGN * KG) void w8_tile_kernel(GemmI8Args a) {
       w[d][n] = __builtin_bit_cast(
           i32x4, __builtin_amdgcn_raw_buffer_load_b128(
                      __builtin_amdgcn_make_buffer_rsrc((void*)wp[SWIGLU ? n & 1 : 0], (short)0, s < KS ? wbytes : 0, 0x00020000),
-                     lane * 16, (t * KS + s) * 1024, 0));
+                     (uint32_t)(lane * 16 + (t * KS + s) * 1024), 0, 0));
     }
   };
 
