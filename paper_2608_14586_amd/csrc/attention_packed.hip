@@ -54,8 +54,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int BKV = 64;
 
-__device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, void* lds, unsigned voff, int soff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, 0);
+// (the row is in the vector offset, which the buffer's range check is sure to count; the scalar one it need not)
+__device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, void* lds, unsigned voff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, voff, 0, 0, 0);
 }
 // every load of this wave has landed, every LDS access is done; then all waves meet
 __device__ __forceinline__ void landed() {
@@ -204,12 +205,12 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attention_packed_kerne
   auto issue_k = [&](char* st, int t) {
     const __amdgpu_buffer_rsrc_t r = rows_at(kh, a.k.token, t);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) dma16(r, st + (wave * LOADS + j) * 1024, kv[j], 0);
+    for (int j = 0; j < LOADS; ++j) dma16(r, st + (wave * LOADS + j) * 1024, kv[j]);
   };
   auto issue_v = [&](char* st, int t) {
     const __amdgpu_buffer_rsrc_t r = rows_at(vh, a.v.token, t);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) dma16(r, st + (wave * LOADS + j) * 1024, vv, (int)(j * RPK * a.v.token * 2));
+    for (int j = 0; j < LOADS; ++j) dma16(r, st + (wave * LOADS + j) * 1024, vv + (unsigned)(j * RPK * a.v.token * 2));
   };
 
   f32x16 acc[ND];

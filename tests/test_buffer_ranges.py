@@ -1,6 +1,7 @@
-"""Loads through buffers in the 8-bit products leave rows and steps past the end to the buffer's range
-check.  That check is sure of the vector offset only (a scalar offset counts towards the address, but a
-check may leave it out, or wrap where it alone lies past the end): so the scalar offset of every such load is 0."""
+"""Loads through buffers in the 8-bit products and in attention over packed prompts leave rows and steps
+past the end to the buffer's range check.  That check is sure of the vector offset only (a scalar offset
+counts towards the address, but a check may leave it out, or wrap where it alone lies past the end): so the
+scalar offset of every such load is 0."""
 import os
 import re
 
@@ -25,7 +26,7 @@ def _arguments(text, at):
             args[-1] += c
 
 
-@pytest.mark.parametrize("name,least", [("w8.hip", 5)])
+@pytest.mark.parametrize("name,least", [("w8.hip", 5), ("attention_packed.hip", 1)])
 def test_no_scalar_offset_decides_a_range(name, least):
     with open(os.path.join(CSRC, name)) as f:
         text = re.sub(r"//.*", "", f.read())
