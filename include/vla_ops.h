@@ -243,8 +243,9 @@ vla_status vla_op_gemm_i8_tile(int M, int N, int K, int tile[2]);
  * offsets[n_seq + 1] (device int32) do not fall; those outside [0, T] are cut.  A
  * prompt may have no rows.  Rows of o in no prompt stay as they were, rows of q, k, v
  * in none may hold anything.  A prompt's results do not depend on the call's others, to
- * the last bit; a key or value that is not finite makes the rows behind it in its prompt
- * not finite (a value: in its dim), and no others.
+ * the last bit.  A value that is not finite makes its own row and those behind it in its prompt not finite in its
+ * dim, a NaN key all of their dims; of an infinite key's scores +inf makes a row NaN, and -inf is no weight (a
+ * row with nothing but such scores is NaN).  No other row is touched.
  * dh in {64, 128}, H % Hkv == 0, token strides below 2^24. */
 vla_status vla_op_attention_packed(const vla_heads *q, const vla_heads *k, const vla_heads *v, const int32_t *offsets,
                                    const vla_heads *o, int n_seq, int T, int H, int Hkv, int dh, void *stream);

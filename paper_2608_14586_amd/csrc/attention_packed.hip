@@ -53,6 +53,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int BKV = 64;
+// A maximum before any score: finite, and below every finite score, so that scores of -inf have the weight 0, also
+// where a query has met no other.  A query that meets none at all has the sum 0, and NaN for a result.
+constexpr float LOWEST = -3e38f;
 
 // (the row is in the vector offset, which the buffer's range check is sure to count; the scalar one it need not)
 __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, void* lds, unsigned voff) {
@@ -218,7 +221,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attention_packed_kerne
   for (int t = 0; t < ND; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m = LOWEST, l = 0.f;
 
   // K tile t + 2 and V tile t + 1 go out at the head of tile t, into the stages that tile t - 1 read last
   issue_k(sk0, 0);
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attention_packed_kerne
     top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2;
     if (__any(top > m + 8.f)) {
       // by the query's own scores alone: its bits do not depend on its neighbours
-      const float mn = top > m + 8.f ? top : m, f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float mn = top > m + 8.f ? top : m, f = __builtin_amdgcn_exp2f(m - mn);
       l *= f;
 #pragma unroll
       for (int t = 0; t < ND; ++t)
