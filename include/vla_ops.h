@@ -278,7 +278,8 @@ vla_status vla_op_kv8_load(const void *cache, const int32_t *start, const int32_
 
 /* vla_op_attention_kv4's attention over the 8-bit cache: the same arguments, window,
  * first tokens, cut lengths and scratch (vla_op_attention_kv8_scratch).  A visible key
- * or value that is NaN gives NaN, one that is not visible reaches nothing. */
+ * or value that is NaN gives NaN, one that is not visible reaches nothing.  A query that is not finite gives NaN
+ * (zeros, if it sees no key), and reaches no other. */
 size_t vla_op_attention_kv8_scratch(int B, int Lq, int H, int Hkv, int dh, int max_len, int window, int sinks);
 vla_status vla_op_attention_kv8(const vla_heads *q, const void *cache, const int32_t *lens, const vla_heads *o, int B,
                                 int Lq, int H, int Hkv, int L_cap, int dh, int max_len, int window, int sinks,

@@ -301,7 +301,9 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
 // queries, they run on one XCD one behind the other and read keys from its L2: 16 tokens
 // of 28 heads over 4 KV heads of 131072 keys 100 -> 75 us against tiles apart.
 
-constexpr float LOWEST = -3e38f;  // a maximum before any score: finite, so that no difference of two is NaN
+// A maximum before any score: finite, so that no difference of two is NaN, and no finite score lies below it, so that only
+// scores of -inf have no weight
+constexpr float LOWEST = -__FLT_MAX__;
 constexpr float RISE = 15.f, PLACE = 7.f;
 constexpr float UNIT = 0x1p-28f;
 
@@ -359,10 +361,14 @@ __device__ __forceinline__ Seen seen_of(const Kv8Attn& a, int len, int row0, int
   return s;
 }
 
-// dims d .. d + 3 of query row gr of a KV head: v / l, zeros where no key was seen
-__device__ __forceinline__ void store_row(const Kv8Attn& a, int b, int hk, int gr, int d, const f32x4& v, float l) {
+// 1 / l: of a query that sees no key (query q of len tokens) zero, of one whose keys all have no weight NaN
+__device__ __forceinline__ float share(const Kv8Attn& a, int len, int q, float l) {
+  return l != 0.f ? (1.f / UNIT) / l : len - a.Lq + q < 0 ? 0.f : __uint_as_float(0x7fc00000u);
+}
+// dims d .. d + 3 of query row gr of a KV head: v / l
+__device__ __forceinline__ void store_row(const Kv8Attn& a, int b, int hk, int gr, int d, int len, const f32x4& v, float l) {
   const int q = div_by(gr, a.by_G);
-  const float f = l == 0.f ? 0.f : (1.f / UNIT) / l;
+  const float f = share(a, len, q, l);
   bf16_t* o = (bf16_t*)a.o.p + b * a.o.seq + q * a.o.token + (hk * a.G + gr - q * a.G) * a.o.head + d;
   *(u32x2*)o = u32x2{pack_bf2(v[0] * f, v[1] * f), pack_bf2(v[2] * f, v[3] * f)};
 }
@@ -560,7 +566,7 @@ __global__ __launch_bounds__(W * 64) void kv8_attention_kernel(Kv8Attn a) {
       for (int e = 0; e < 4; ++e) v[e] = fmaf(f, x[e], v[e]);
     }
     if (sn.nb <= a.chunk) {
-      store_row(a, b, hk, gr, d, v, ls);
+      store_row(a, b, hk, gr, d, len, v, ls);
     } else {
       const size_t at = ((size_t)bh * rows + gr) * a.nsplit + split;
       const size_t ml = (size_t)total * rows * a.nsplit * DH + at * 2;
@@ -600,8 +606,8 @@ __global__ __launch_bounds__(64) void kv8_combine_kernel(Kv8Attn a, int total) {
   load(0, a.nsplit);  // what was not written is not used
   const int length = a.lens[b];
   __builtin_amdgcn_sched_barrier(0);
-  const int row0 = gr / TILE * TILE;
-  const Seen sn = seen_of(a, min(max(length, 0), a.max_len), row0, min(rows, row0 + TILE) - 1);
+  const int row0 = gr / TILE * TILE, len = min(max(length, 0), a.max_len);
+  const Seen sn = seen_of(a, len, row0, min(rows, row0 + TILE) - 1);
   const int ns = div_by(sn.nb + a.chunk - 1, a.by_chunk);
   float mx = LOWEST, l = 0.f;
   vec v = {};
@@ -625,7 +631,7 @@ __global__ __launch_bounds__(64) void kv8_combine_kernel(Kv8Attn a, int total) {
   }
   if (ns < 2) return;  // written by the one split
   const int q = div_by(gr, a.by_G);
-  const float f = l == 0.f ? 0.f : (1.f / UNIT) / l;
+  const float f = share(a, len, q, l);
   bf16_t* o = (bf16_t*)a.o.p + b * a.o.seq + q * a.o.token + (hk * a.G + gr - q * a.G) * a.o.head + lane * D;
   if constexpr (D == 2)
     *(uint32_t*)o = pack_bf2(v[0] * f, v[1] * f);
