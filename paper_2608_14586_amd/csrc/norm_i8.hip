@@ -147,7 +147,12 @@ __global__ __launch_bounds__(T) void norm_i8_kernel(NormI8Args p) {
   }
   if (tid == 0) {
     float s = a * (1.f / 127.f);
-    if (NORM && a > 0.f) s *= again ? (float)(1.0 / sqrt(sq / p.d + (double)p.eps)) : 1.f / sqrtf(ss / (float)p.d + p.eps);
+    if (NORM && a > 0.f) {
+      if (again)  // the factor alone may leave fp32, the scale does not for it
+        s = (float)(s / sqrt(sq / p.d + (double)p.eps));
+      else
+        s *= 1.f / sqrtf(ss / (float)p.d + p.eps);
+    }
     p.scales[row] = finite ? s : __uint_as_float(0x7fc00000u);
   }
 #pragma unroll
