@@ -263,8 +263,9 @@ vla_status vla_op_attention_packed(const vla_heads *q, const vla_heads *k, const
  * rounded to it; so the rows ahead of the stored ones in their block must have been
  * stored before.  Codes are rounded to the nearest, ties to even; a value that is not
  * finite is held as NaN and does not move e.
- * load takes rows out into k, v, 2^e c rounded to bf16 (exact).  Positions outside [0, L_cap) are
- * left out; other blocks of the cache (store) and rows of k, v (load) stay as they were.
+ * load takes rows out into k, v, 2^e c rounded to bf16: exact, but where c 2^e is 2^128, which is what values of
+ * 248 2^120 (3.3e38) and above are rounded to; they load as infinity, and count as 2^128 in attention.
+ * Positions outside [0, L_cap) are left out; other blocks of the cache (store) and rows of k, v (load) stay as they were.
  * Prompts packed behind one another are stored in one call as sequences that share
  * all rows: seq 0, start[b] = -offsets[b], count[b] = offsets[b + 1].
  * A call may touch one sequence's slot once; calls on one cache must be ordered

@@ -244,7 +244,7 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
   const int tid = threadIdx.x;
   const u32x4 own = image[tid];
   const Heads& out = values ? a.v : a.k;
-  // four codes as bf16: exact, the codes have 4 bits and a power of two keeps them
+  // four codes as bf16: exact, the codes have 4 bits and a power of two keeps them (256 2^120 alone is infinite)
   auto wide = [&](uint32_t w) {
     const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     return u32x2{pack_bf2(p[0] * step, p[1] * step), pack_bf2(q[0] * step, q[1] * step)};
