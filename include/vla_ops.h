@@ -223,7 +223,7 @@ vla_status vla_op_w8_pack(const void *codes, const float *scales, void *Wp, int 
 
 /* out[M][N] = sx[m] * scales[n] * sum_k x[m][k] codes[n][k] + residual[M][N] (fp32,
  * NULL = none), x[M][K] int8 with a scale a row, sx[M] (fp32), W the packed 8-bit
- * weights, out in out_dtype.  The sum is exact, whatever M.
+ * weights, out in out_dtype.  The sum is exact, whatever M; its factors follow one by one in fp32, sx first.
  * swiglu: W holds N / 2 gate rows, then the N / 2 up rows, and out[M][N / 2] =
  * silu(x Wgate^T) * (x Wup^T) + residual; N % 64 == 0.
  * Row strides in elements, no less than a row's width where M > 1: ldx of x (a
@@ -267,7 +267,8 @@ vla_status vla_op_attention_packed(const vla_heads *q, const vla_heads *k, const
  * 248 2^120 (3.3e38) and above are rounded to; they load as infinity, and count as 2^128 in attention.
  * Positions outside [0, L_cap) are left out; other blocks of the cache (store) and rows of k, v (load) stay as they were.
  * Prompts packed behind one another are stored in one call as sequences that share
- * all rows: seq 0, start[b] = -offsets[b], count[b] = offsets[b + 1].
+ * all rows: seq 0, start[b] = -offsets[b], count[b] = offsets[b + 1].  Such a call looks at B (L / 32 + 2) blocks a
+ * head, most of them without rows.
  * A call may touch one sequence's slot once; calls on one cache must be ordered
  * (one stream).  L_cap % 32 == 0, L_cap <= 2^24, dh in {64, 128}.
  * vla_op_kv8_bytes is 0 for sizes that are refused. */

@@ -13,14 +13,17 @@
 // weights are the operand of O^T = V^T P^T as they lie, for the keys 16 s + 4 h + j and 16 s
 // + 8 + 4 h + j (h = lane / 32, j < 4) of each k-step.  V's operand, those keys of one dim,
 // is read with a transposing LDS load (ds_read_b64_tr_b16: four keys of 16 dims a group
-// of 16 lanes), so nothing is transposed beforehand.  The sum is of the rounded weights,
-// two a v_dot2, so weights and sum are rounded alike.
+// of 16 lanes), so nothing is transposed beforehand.  Weights are rounded to bf16, since values are bf16
+// and an MFMA's operands of one type: 2^-8 of each at most, and 0.0019 to 0.0020 of the result against 64 bits, where its
+// own rounding alone gives 0.0016.  The sum is of the rounded weights, two a v_dot2, so both are rounded alike.
 //
 // A wave works one tile ahead: between the exponentials of tile t its MFMAs form the
-// scores of tile t + 1.  One long prompt (16384 tokens, 8 heads of 128) takes 520 us, 1060
-// TF/s of the half that is not masked: the matrix cores are busy for 62% of the cycles, at
-// the 1.6 GHz that the chip holds under it.  Four prompts of 4096, 2048, 1201 and 847, 32 heads:
-// 202 to 225 us.  With less to do a tile takes a workgroup that has a CU alone 1.05 us, its
+// scores of tile t + 1.  One long prompt (16384 tokens, 8 heads of 128) takes 530 to 545 us, 1010 to
+// 1040 TF/s of the half that is not masked, four prompts of 4096, 2048, 1201 and 847, 32 heads, 217 to 222: the matrix cores
+// are busy for 52% and 42% of the cycles, at the 1.7 to 1.95 GHz that the chip holds under it.  Their operands, 1 KB from
+// LDS for each MFMA of 32 cycles, take as long at 128 bytes a cycle (no bank conflicts), and so do exponentials and what else the
+// softmax asks of the vector unit, by instruction counts; a SIMD's two waves overlap the three in part.  One prompt of
+// 2048, 32 heads: 48 us (attention_bf16.hip, whose values come transposed, 43 to 45).  With less to do a tile takes a workgroup that has a CU alone 1.05 us, its
 // parts one behind the other: without the loads 0.93, without exponentials 1.0, without
 // three quarters of the PV products 1.0.  What did not help: 64 queries a wave (half the LDS reads,
 // but 268 us for 225: accumulators wander between the register files), the next tile's maximum and

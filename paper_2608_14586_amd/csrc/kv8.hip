@@ -84,7 +84,9 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
 // 2048 tokens of 32 heads of 128, 50 MB in all, take 13.1 us (3.8 TB/s, the launch's 2.3 us
 // included), a token of each of four sequences of two heads 3.3.  Values transposed in
 // registers and all rows in whole cache lines through LDS measured 13.2 us, keys and values
-// in one workgroup 13.7 and 3.9.
+// in one workgroup 13.7 and 3.9.  Sequences that share all rows have a workgroup for each block that any of
+// them might touch: 12 prompts in 8192 rows, 32 heads of 128, 104 us where one sequence of 8192 takes 42, 64
+// prompts, 8 heads, 109 for 12.
 template <int DH>
 __global__ __launch_bounds__(2 * DH) void kv8_store_kernel(Kv8Rows a) {
   constexpr int T = 2 * DH, W = T / 64, TPR = T / BLK, V = DH / TPR;  // threads a row, values a thread: 16
@@ -283,19 +285,21 @@ __global__ __launch_bounds__(2 * DH) void kv8_load_kernel(Kv8Rows a) {
 //    that a lane holds 8 keys of one query; the block's step and 1 / sqrt(dh) are one
 //    factor a block;
 //  * softmax: a running maximum and sum a query in fp32, one pass.  The maximum moves only
-//    where a score is 15 (in log2) above it, to 7 above the score: weights lie below 2^15 and are
-//    rounded to fp16, 2^-12 of each, and what falls below fp16's range is less than 2^-31 of the largest;
+//    where a score is 15 (in log2) above it, to 7 below the score: weights lie below 2^15 and are
+//    rounded to fp16, off by 2^-11 of each at most (below fp16's normal range by 2^-32 of the largest), an eighth of
+//    what the bf16 result's own rounding may be;
 //  * O^T = V^T P^T by fp16 MFMA: a lane's 8 weights are the operand as they lie, value
 //    codes are fp16 numbers exactly; the block's step is a factor of the block's sum, in
 //    fp32, so that no block's step limits another's.  It comes in as 2^-28 of itself:
-//    sums of values near the largest bf16 stay in range, and the last factor takes it back.
+//    sums of values near the largest bf16 stay in range, as long as weights add up to less than 2^28: over 8192 keys
+//    whatever their scores, over 2^21 whose scores lie below the first maximum.  The last factor takes it back.
 // A key that a query does not see has the score -inf and the weight 0.  Values that no
 // query of the tile sees are taken as zero codes.  A NaN among values that some of its queries see
 // and others do not must reach the former only: 0 NaN is NaN, so such codes are zeroed
 // too, and a product of (is NaN) with (sees it) marks the outputs that they make NaN.
 // Work is split over the keys: waves of a workgroup take every W-th block, workgroups
 // contiguous runs of blocks, joined in LDS and by kv8_combine_kernel.  Reading the cache
-// bounds it: a token of 16 sequences of 32768 over 8 KV heads of 128 takes 186 us (5.8 TB/s), of
+// bounds it: a token of 16 sequences of 32768 over 8 KV heads of 128 takes 185 to 195 us (5.5 to 5.8 TB/s), of
 // eight of 4096 to 32768 63 (4.8 TB/s: lengths are not known where work is split), of one
 // of 2048 over 32 heads 9.1, of which 4.6 are two launches.  Where a KV head has several tiles of
 // queries, they run on one XCD one behind the other and read keys from its L2: 16 tokens

@@ -431,12 +431,13 @@ hipError_t launch_rows(const GemmI8Args& a, hipStream_t s) {
 // products timed in every tile with their weights read from memory (M = 17 to 4096, N =
 // 256 to 22016, K = 256 to 11008; mean error 9 to 13%); what the choice takes is
 // 1.8% slower than the fastest tile on average, 23% in one of a hundred, 39% at most.  us,
-// the same four products in each tile (- : not timed):
+// the same products in each tile:
 //                                        128x512 128x256 64x256 128x128 64x128 48x128 64x64 32x64 32x32
-//   2048 x 22016, K =  4096, gated            161     167    218     191    261      -   286     -     -
-//   2048 x 12288, K =  4096                   110      91    123     107    146      -   163     -     -
-//    333 x  4096, K = 11008, residual         115      68     56      48     35     36    42    50    60
-//     64 x  4096, K = 11008, residual          95      53     40      33     28     24    20    15    14 (from cache)
+//   2048 x 22016, K =  4096, gated            160     161    206     185    242    252   273   407   464 (from cache)
+//   2048 x 12288, K =  4096                   107      92    128     111    149    153   165   236   268
+//    333 x  4096, K = 11008, residual         121      72     58      51     37     37    43    50    62
+//    333 x  4096, K = 11008, residual          98      55     40      39     29     26    33    38    52 (from cache)
+//     64 x  4096, K = 11008, residual          93      51     40      32     27     24    20    16    14 (from cache)
 struct Tile {
   int rows, cols, per_cu;
   float t0, t1, step, t2, t3, f;
@@ -507,9 +508,13 @@ void gemm_i8_tile(int M, int N, int K, int* rows, int* cols) {
 
 hipError_t gemm_i8(const GemmI8Args& a, hipStream_t s) {
   if (a.M <= 16) {
-    // waves and tiles a workgroup by the number of tiles.  us, one row, weights from memory, 8 waves, 4 waves, 4 waves
-    // of two tiles: N = 4096, K = 4096 5.7, 6.2, 7.2; N = 12288 11.4, 11.1, 12.1; 16 rows, N = 57344, K = 8192 110, 107, and 90
-    // as 8 waves of two tiles
+    // waves and tiles a workgroup by the number of tiles.  us, weights from memory, of one row (of 16): 8 waves, 4 waves, 8
+    // waves of two tiles
+    //    2048, K = 2048   3.0  3.5  3.6 ( 3.6  4.1  4.2)      12288, K = 4096  11.4 11.4 12.1 (14.2 13.9 13.4)
+    //    4096, K = 4096   5.8  6.5  6.3 ( 6.6  7.2  7.6)      16416, K = 4096  15.1 14.7 15.5 (19.3 19.7 17.7)
+    //    8192, K = 4096   8.6  8.4  8.4 (10.0 10.3  9.1)      22016, K = 4096  18.6 18.4 17.7 (25.0 25.5 20.1)
+    //    8224, K = 4096  10.0  9.8 10.6 (12.6 12.6 12.2)      57344, K = 8192  78   79   77   ( 111  112   86)
+    // What lies between is flat for one row; with 16 two tiles are faster from N = 6144 on.
     if (a.swiglu) return launch_rows<2, 8, 2>(a, s);
     return a.N <= 8192    ? launch_rows<1, 8, 4>(a, s)
            : a.N <= 16384 ? launch_rows<1, 4, 4>(a, s)
